@@ -22,6 +22,9 @@
  *                                                               (Algorithm 2, inner repeat)
  *   skim_cluster_rows_exact  the optimum of the clustering objective per row (yardstick for the iterations)
  *   skim_scale_update_lfull  the same Adam steps on the L-full loss      (Section 4.3; Section 3.4)
+ *   skim_grouped_quantize, skim_grouped_dequantize, skim_grouped_matvec, skim_grouped_gated   uniform 4-bit weights with a scale per
+ *                         group of columns, which the paper compares its codebooks with, and their products with token rows
+ *   skim_add_rmsnorm      the norm in front of those products, with 16-bit or 8-bit rows as its result
  *   skim_residual, skim_err_lfull   the error of a row in the L-full form, (w - wq) X X^T (w - wq)^T
  *                                                               (Section 3.4; Section 4.2; Algorithm 3)
  *
@@ -69,6 +72,8 @@ extern "C" {
 #define SKIM_ERR_SCALE (-8)       /* installed scale vector length differs from cols */
 #define SKIM_ERR_ALIGN (-9)       /* an output pointer is not aligned as documented */
 #define SKIM_ERR_STATIC_LIMIT (-10) /* skim_quantize_static: rows above SKIM_STATIC_MAX_ROWS */
+
+#define SKIM_ERR_TYPE (-11)       /* an element type, group size or activation that the call does not take */
 
 #define SKIM_MAX_BIT 4            /* the paper caps the width at 4 bits (Section 5.1) */
 
@@ -286,6 +291,74 @@ int skim_dequantize(skim_ctx *ctx, const uint32_t *packed, const int32_t *row_or
 int skim_matvec(skim_ctx *ctx, const uint32_t *packed, const int32_t *row_order, const int64_t *group_info,
                 const uint16_t *lut, const float *s, const uint16_t *x, int64_t rows, int64_t cols,
                 const int *bit_set, int n_bits, float *y);
+
+/* Element types and activations of the calls below. */
+#define SKIM_TYPE_F16 0
+#define SKIM_TYPE_BF16 1
+#define SKIM_TYPE_F32 2
+#define SKIM_TYPE_I8 3
+#define SKIM_ACT_SILU 0           /* g / (1 + exp(-g)) */
+#define SKIM_ACT_GELU 1           /* 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) */
+#define SKIM_MAX_TOKENS 1048560   /* token rows of one call */
+#define SKIM_MAX_GROUPED_COLS 16777216
+
+/*
+ * Uniform 4-bit quantisation with group scales: the form the paper's codebooks are compared with (the baselines of its
+ * tables).  `group` (32, 64 or 128) neighbouring columns of a row share a scale and a zero point (the last group of a row may be shorter):
+ *   low = min(0, min x), high = max(0, max x);  s = binary16(binary32(binary32(high - low) / 15))
+ *   z = clamp(rint(-low / s), 0, 15),  code = clamp(rint(x / s) + z, 0, 15)   (ties to even; s = 0: z = 0 and all codes 0)
+ *   the value that a code stands for is (code - z) * s.
+ * x is the value that the clustering clusters: float(W), or its binary32 product with the installed scale vector's reciprocal (SKIM_ERR_SCALE
+ * where its length differs); the products below then take activations times alpha.
+ *   tiles  out, 16-byte aligned, skim_grouped_bytes bytes, all of them written: records of 16 rows x 128 columns, one row of records after
+ *          another, rows and columns beyond the matrix zero.  A record is 256 words of codes -- word 16 i + 4 p + t: row i, columns
+ *          32 t + 8 p + e (e < 8), column e in nibble 4 (e & 1) + e / 2 -- and behind them a word for every row and group (row-major): the
+ *          scale's 16 bits, the zero point in the byte above them.
+ *   err    out [rows] binary32, may be NULL: sum_j g_ij (x_ij - value_ij)^2 with g the importance (same layout as W; NULL: 1), the
+ *          objective that skim_cluster_rows reports.  Summed in binary32 in a fixed order.
+ * Needs a workspace of 512 bytes (status word): NaN or Inf in W sets SKIM_STATUS_BAD_WEIGHT, and SKIM_STATUS_BAD_IMPORTANCE as in the clustering.
+ * skim_grouped_bytes is a host-only helper.
+ */
+int skim_grouped_bytes(int64_t rows, int64_t cols, int group, size_t *out);
+int skim_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *importance, int64_t rows, int64_t cols, int64_t ld, int group,
+                          void *tiles, float *err);
+/* out [rows][ld_out] binary16: the values, rounded once.  No workspace is used. */
+int skim_grouped_dequantize(skim_ctx *ctx, const void *tiles, int64_t rows, int64_t cols, int group, uint16_t *out, int64_t ld_out);
+
+/*
+ * y[t][i] = xs[t] * sum_j value_ij x[t][j] for token rows x [tokens][ldx], straight from the stored form.
+ *   x        SKIM_TYPE_F16, SKIM_TYPE_BF16 or SKIM_TYPE_I8 elements
+ *   x_scale  [tokens] binary32: xs, or NULL (1).  8-bit rows and their scales come from skim_add_rmsnorm.
+ *   y        out [tokens][ldy] SKIM_TYPE_F32, SKIM_TYPE_F16 or SKIM_TYPE_BF16 elements, each rounded once
+ * Codes less zero points, and 8-bit activations, enter the tensor cores as exact numbers; products are exact; a group's sum and the sum over the
+ * groups, each group taken times its scale, are binary32.  The values themselves are never rounded to 16 bits.
+ * (A partial sum of |code - z| |x| over a group has to stay in the binary32 range.)
+ *
+ * skim_grouped_gated: y = act(gate x) * (up x), both matrices [rows][cols] in the stored form with the same group size, in one kernel.
+ *
+ * rows, tokens >= 0 (0 is a no-op), 1 <= cols <= SKIM_MAX_GROUPED_COLS.  ldx >= cols, ldy >= rows.  Matrices are 16-byte aligned; x and y need the
+ * alignment of their elements only (rows of x at multiples of 16 bytes -- 8 for 8-bit rows -- are faster).  y must not overlap x.
+ * Needs a workspace of 512 bytes (status word: SKIM_STATUS_TIMEOUT).  Same inputs, same bits, on every run.
+ */
+int skim_grouped_matvec(skim_ctx *ctx, const void *tiles, int64_t rows, int64_t cols, int group, const void *x, int x_type, int64_t ldx,
+                        const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy);
+int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t rows, int64_t cols, int group, int activation,
+                       const void *x, int x_type, int64_t ldx, const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy);
+
+/*
+ * The residual's addition and the root-mean-square norm of token rows:
+ *   h = x + residual (binary32; residual may be NULL);  rstd = 1 / sqrt(sum_j h_j^2 / cols + eps);  p = binary32(h * weight) (weight [cols] may
+ *   be NULL: 1).  x, residual, weight and sum_out have elements of `type`, SKIM_TYPE_F16 or SKIM_TYPE_BF16.
+ *   sum_out    out, may be NULL: h rounded to `type`, the new residual stream
+ *   out        out, out_type == type: p * rstd, rounded once; out_type == SKIM_TYPE_I8: codes rint(127 p / a), a = max_j |p_j| of the
+ *              row, decided as by the exact quotient (ties to even), standing for code * out_scale
+ *   out_scale  out [rows] binary32, SKIM_TYPE_I8 only: a * rstd / 127.  A row that holds a value that is not finite gets a scale that is NaN or Inf;
+ *              its codes are in range, 0 where the quotient is not a number.
+ * Sums of squares are binary32.  sum_out may be x or residual, and a 16-bit out may be x or residual where sum_out is not the same (same pointer and stride);
+ * no other overlap.  rows >= 0 (0 is a no-op), 1 <= cols <= SKIM_MAX_GROUPED_COLS, strides (elements) >= cols, eps finite and >= 0.  No workspace is used.
+ */
+int skim_add_rmsnorm(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int type, int64_t rows,
+                     int64_t cols, float eps, void *sum_out, int64_t lds, void *out, int out_type, int64_t ldo, float *out_scale);
 
 /*
  * Algorithm 2, inner repeat: `steps` Adam updates (Section 5.1: learning rate lr0, multiplied

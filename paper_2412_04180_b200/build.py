@@ -10,7 +10,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libskim.so")
 LIB_CHECKED = os.path.join(HERE, "libskim_checked.so")   # the same sources with -DSKIM_CHECK_BOUNDS
-SOURCES = ["skim_api.cu", "skim_cluster.cu", "skim_cluster16.cu", "skim_bucket.cu", "skim_lloyd.cu", "skim_allocate.cu", "skim_quantize.cu", "skim_unpack.cu", "skim_scale.cu", "skim_lfull.cu", "skim_exact.cu"]
+SOURCES = ["skim_api.cu", "skim_cluster.cu", "skim_cluster16.cu", "skim_bucket.cu", "skim_lloyd.cu", "skim_allocate.cu", "skim_quantize.cu", "skim_unpack.cu", "skim_scale.cu", "skim_lfull.cu", "skim_exact.cu",
+           "skim_grouped.cu", "skim_grouped_small.cu", "skim_norm.cu"]
 
 
 def _stale(lib=LIB) -> bool:
@@ -29,7 +30,7 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     if not force and not _stale(lib):
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
+    cmd = [nvcc, "-std=c++17", "-O3", "--threads", "0", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
            "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
            "-o", lib] + [os.path.join(CSRC, s) for s in SOURCES]
     if checked:

@@ -2,7 +2,7 @@
 #include <math.h>
 #include <new>
 
-#include "skim_internal.cuh"
+#include "skim_grouped.cuh"
 
 int skim_check_bits(const int *bit_set, int n_bits, SkimBits *out)
 {
@@ -679,6 +679,125 @@ int skim_lloyd_iterations(skim_ctx *ctx, int64_t *iterations, int64_t *rows)
     return SKIM_OK;
 }
 
+// ---------------------------------------------------------------- group scales and the norm in front of them
+
+namespace {
+
+int check_grouped(const void *tiles, int64_t rows, int64_t cols, int group)
+{
+    if (group != 32 && group != 64 && group != 128) return SKIM_ERR_TYPE;
+    if (rows < 0 || rows > 0x7fffffff || cols < 1 || cols > SKIM_MAX_GROUPED_COLS) return SKIM_ERR_SHAPE;
+    return (reinterpret_cast<uintptr_t>(tiles) & 15u) ? SKIM_ERR_ALIGN : SKIM_OK;
+}
+unsigned type_bytes(int type) { return type == SKIM_TYPE_F32 ? 4u : type == SKIM_TYPE_I8 ? 1u : 2u; }
+bool aligned_for(const void *p, int type) { return reinterpret_cast<uintptr_t>(p) % type_bytes(type) == 0; }
+
+int grouped_product(skim_ctx *ctx, const SkimGroupedProduct &p)
+{
+    const bool none = p.rows == 0 || p.tokens == 0;           // empty arrays may have no address
+    if (!ctx || (!none && (!p.tiles[0] || (p.gated && !p.tiles[1]) || !p.x || !p.out))) return SKIM_ERR_NULL;
+    if (p.x_type != SKIM_TYPE_F16 && p.x_type != SKIM_TYPE_BF16 && p.x_type != SKIM_TYPE_I8) return SKIM_ERR_TYPE;
+    if (p.out_type != SKIM_TYPE_F16 && p.out_type != SKIM_TYPE_BF16 && p.out_type != SKIM_TYPE_F32) return SKIM_ERR_TYPE;
+    if (p.gated && p.act != SKIM_ACT_SILU && p.act != SKIM_ACT_GELU) return SKIM_ERR_TYPE;
+    int rc = check_grouped(p.tiles[0], p.rows, p.cols, p.group);
+    if (!rc && p.gated) rc = check_grouped(p.tiles[1], p.rows, p.cols, p.group);
+    if (rc) return rc;
+    if (p.tokens < 0 || p.tokens > SKIM_MAX_TOKENS || p.ldx < p.cols || p.ldo < p.rows) return SKIM_ERR_SHAPE;
+    if (!aligned_for(p.x, p.x_type) || !aligned_for(p.out, p.out_type) || !aligned_for(p.x_scale, SKIM_TYPE_F32)) return SKIM_ERR_ALIGN;
+    if (!ctx->ws) return SKIM_ERR_WORKSPACE;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SKIM_ERR_CUDA;
+    SkimGroupedProduct q = p;
+    q.status = (unsigned long long *)ctx->ws;
+    return skim_launch_grouped_small(ctx, q);
+}
+
+}  // namespace
+
+int skim_grouped_bytes(int64_t rows, int64_t cols, int group, size_t *out)
+{
+    if (!out) return SKIM_ERR_NULL;
+    const int rc = check_grouped(nullptr, rows, cols, group);
+    if (rc) return rc;
+    *out = (size_t)skim_record_tiles(rows, SKIM_RECORD_ROWS) * (size_t)skim_record_tiles(cols, SKIM_RECORD_COLS) * (size_t)skim_record_bytes(group);
+    return SKIM_OK;
+}
+
+int skim_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *importance, int64_t rows, int64_t cols, int64_t ld, int group,
+                          void *tiles, float *err)
+{
+    if (!ctx || (rows != 0 && (!W || !tiles))) return SKIM_ERR_NULL;
+    const int rc = check_grouped(tiles, rows, cols, group);
+    if (rc) return rc;
+    if (ld < cols) return SKIM_ERR_SHAPE;
+    if (!aligned_for(W, SKIM_TYPE_F16) || !aligned_for(importance, SKIM_TYPE_F32) || !aligned_for(err, SKIM_TYPE_F32)) return SKIM_ERR_ALIGN;
+    if (!ctx->ws) return SKIM_ERR_WORKSPACE;
+    if (ctx->scaled && ctx->scale_cols != cols) return SKIM_ERR_SCALE;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SKIM_ERR_CUDA;
+    return skim_launch_grouped_quantize(ctx, W, importance, ctx->scaled ? skim_carve(ctx->ws, 0, cols).rscale : nullptr, rows, cols, ld, group,
+                                        static_cast<unsigned char *>(tiles), err);
+}
+
+int skim_grouped_dequantize(skim_ctx *ctx, const void *tiles, int64_t rows, int64_t cols, int group, uint16_t *out, int64_t ld_out)
+{
+    if (!ctx || (rows != 0 && (!tiles || !out))) return SKIM_ERR_NULL;
+    const int rc = check_grouped(tiles, rows, cols, group);
+    if (rc) return rc;
+    if (ld_out < cols) return SKIM_ERR_SHAPE;
+    if (!aligned_for(out, SKIM_TYPE_F16)) return SKIM_ERR_ALIGN;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SKIM_ERR_CUDA;
+    return skim_launch_grouped_dequantize(ctx, static_cast<const unsigned char *>(tiles), rows, cols, group, out, ld_out);
+}
+
+int skim_grouped_matvec(skim_ctx *ctx, const void *tiles, int64_t rows, int64_t cols, int group, const void *x, int x_type, int64_t ldx,
+                        const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy)
+{
+    SkimGroupedProduct p = {};
+    p.tiles[0] = static_cast<const unsigned char *>(tiles);
+    p.rows = rows; p.cols = cols; p.group = group;
+    p.x = x; p.x_type = x_type; p.ldx = ldx; p.x_scale = x_scale; p.tokens = tokens;
+    p.out = y; p.out_type = y_type; p.ldo = ldy;
+    return grouped_product(ctx, p);
+}
+
+int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t rows, int64_t cols, int group, int activation,
+                       const void *x, int x_type, int64_t ldx, const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy)
+{
+    SkimGroupedProduct p = {};
+    p.tiles[0] = static_cast<const unsigned char *>(gate);
+    p.tiles[1] = static_cast<const unsigned char *>(up);
+    p.gated = 1; p.act = activation;
+    p.rows = rows; p.cols = cols; p.group = group;
+    p.x = x; p.x_type = x_type; p.ldx = ldx; p.x_scale = x_scale; p.tokens = tokens;
+    p.out = y; p.out_type = y_type; p.ldo = ldy;
+    return grouped_product(ctx, p);
+}
+
+int skim_add_rmsnorm(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int type, int64_t rows,
+                     int64_t cols, float eps, void *sum_out, int64_t lds, void *out, int out_type, int64_t ldo, float *out_scale)
+{
+    if (!ctx || (rows != 0 && (!x || !out))) return SKIM_ERR_NULL;
+    if (type != SKIM_TYPE_F16 && type != SKIM_TYPE_BF16) return SKIM_ERR_TYPE;
+    if (out_type != type && out_type != SKIM_TYPE_I8) return SKIM_ERR_TYPE;
+    if (rows != 0 && out_type == SKIM_TYPE_I8 && !out_scale) return SKIM_ERR_NULL;
+    if (rows < 0 || rows > 0x7fffffff || cols < 1 || cols > SKIM_MAX_GROUPED_COLS || ldx < cols || ldo < cols || (residual && ldr < cols) ||
+        (sum_out && lds < cols) || !(eps >= 0.0f && eps <= 3.402823466e38f))
+        return SKIM_ERR_SHAPE;
+    if (!aligned_for(x, type) || !aligned_for(residual, type) || !aligned_for(weight, type) || !aligned_for(sum_out, type) || !aligned_for(out, out_type) ||
+        !aligned_for(out_scale, SKIM_TYPE_F32))
+        return SKIM_ERR_ALIGN;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return SKIM_ERR_CUDA;
+    SkimNorm n = {};
+    n.x = x; n.residual = residual; n.weight = weight; n.type = type;
+    n.rows = rows; n.cols = cols; n.ldx = ldx; n.ldr = ldr; n.lds = lds; n.ldo = ldo;
+    n.eps = eps; n.sum_out = sum_out; n.out = out; n.out_type = out_type;
+    n.out_scale = out_type == SKIM_TYPE_I8 ? out_scale : nullptr;
+    return skim_launch_add_rmsnorm(ctx, n);
+}
+
 const char *skim_strerror(int code)
 {
     switch (code) {
@@ -693,6 +812,7 @@ const char *skim_strerror(int code)
     case SKIM_ERR_SCALE: return "installed scale vector length differs from cols";
     case SKIM_ERR_ALIGN: return "output pointer not aligned as documented";
     case SKIM_ERR_STATIC_LIMIT: return "skim_quantize_static: rows exceed SKIM_STATIC_MAX_ROWS (65536), the size of the built-in scratch array";
+    case SKIM_ERR_TYPE: return "element type, group size or activation not among those the call takes";
     default: return "unknown error";
     }
 }

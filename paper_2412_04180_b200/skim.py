@@ -19,13 +19,20 @@ _lib = None
 
 ERR_NAMES = {0: "SKIM_OK", -1: "SKIM_ERR_NULL", -2: "SKIM_ERR_SHAPE", -3: "SKIM_ERR_BITSET",
              -4: "SKIM_ERR_BUDGET", -5: "SKIM_ERR_WORKSPACE", -6: "SKIM_ERR_CUDA",
-             -7: "SKIM_ERR_BAD_DATA", -8: "SKIM_ERR_SCALE", -9: "SKIM_ERR_ALIGN", -10: "SKIM_ERR_STATIC_LIMIT"}
+             -7: "SKIM_ERR_BAD_DATA", -8: "SKIM_ERR_SCALE", -9: "SKIM_ERR_ALIGN", -10: "SKIM_ERR_STATIC_LIMIT",
+             -11: "SKIM_ERR_TYPE"}
 
 EXPORTS = ["skim_create", "skim_destroy", "skim_max_cols", "skim_workspace_bytes", "skim_set_workspace",
            "skim_apply_scale", "skim_cluster_rows", "skim_cluster_rows_at", "skim_cluster_exact_bytes", "skim_cluster_rows_exact", "skim_allocate_bits", "skim_allocate_bits_floor", "skim_allocate_bits_until", "skim_allocate_optimal_bytes", "skim_allocate_optimal",
            "skim_packed_layout", "skim_quantize", "skim_quantize_static", "skim_dequantize", "skim_matvec", "skim_scale_update", "skim_scale_lfull_bytes", "skim_scale_update_lfull", "skim_residual", "skim_err_lfull_bytes", "skim_err_lfull", "skim_host_staging_bytes",
            "skim_quantize_matrix_host", "skim_get_status", "skim_launch_count", "skim_kernel_timing",
-           "skim_kernel_times", "skim_early_exit", "skim_lloyd_iterations", "skim_strerror"]
+           "skim_kernel_times", "skim_early_exit", "skim_lloyd_iterations", "skim_strerror",
+           "skim_grouped_bytes", "skim_grouped_quantize", "skim_grouped_dequantize", "skim_grouped_matvec", "skim_grouped_gated",
+           "skim_add_rmsnorm"]
+
+# element types and activations of the products with grouped weights and of the norm
+TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2, torch.int8: 3}
+ACTIVATIONS = {"silu": 0, "gelu": 1}
 
 
 class SkimError(RuntimeError):
@@ -52,6 +59,13 @@ def lib():
         vp, i64 = C.c_void_p, C.c_int64
         _lib.skim_dequantize.argtypes = [vp] * 6 + [i64, i64, vp, C.c_int, vp, i64]
         _lib.skim_matvec.argtypes = [vp] * 7 + [i64, i64, vp, C.c_int, vp]
+        i32 = C.c_int
+        _lib.skim_grouped_bytes.argtypes = [i64, i64, i32, vp]
+        _lib.skim_grouped_quantize.argtypes = [vp] * 3 + [i64, i64, i64, i32, vp, vp]
+        _lib.skim_grouped_dequantize.argtypes = [vp, vp, i64, i64, i32, vp, i64]
+        _lib.skim_grouped_matvec.argtypes = [vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, i64]
+        _lib.skim_grouped_gated.argtypes = [vp, vp, vp, i64, i64, i32, i32, vp, i32, i64, vp, i64, vp, i32, i64]
+        _lib.skim_add_rmsnorm.argtypes = [vp, vp, i64, vp, i64, vp, i32, i64, i64, C.c_float, vp, i64, vp, i32, i64, vp]
     return _lib
 
 
@@ -295,6 +309,151 @@ class Skim:
                                q["lut"].data_ptr(), None if s is None else s.data_ptr(), x.data_ptr(), rows, cols, arr, nb,
                                out.data_ptr()), "skim_matvec")
         return out
+
+    # ---- weights of 4 bits with group scales, their products with token rows, and the norm in front of them
+    def _new(self, shape, dtype):
+        """A tensor of the context's device, made on the context's stream (which writes it)."""
+        if self._stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self._stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _rows_of(self, t, name, dtypes, cols=None):
+        """(rows, stride in elements) of a matrix, or of a vector as one row; elements of a row lie side by side."""
+        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype in dtypes):
+            raise TypeError(f"{name}: expected a tensor on {self.device} of dtype {' or '.join(str(d) for d in dtypes)}")
+        shape = t.shape
+        if not 1 <= len(shape) <= 2 or (cols is not None and shape[-1] != cols):
+            raise TypeError(f"{name}: expected a vector or a matrix" + ("" if cols is None else f" of {cols} columns") + f", got shape {tuple(shape)}")
+        rows = shape[0] if len(shape) == 2 else 1
+        if t.stride(-1) != 1 and shape[-1] > 1:
+            raise TypeError(f"{name}: the elements of a row have to lie side by side")
+        if rows <= 1:
+            return rows, shape[-1]
+        return rows, t.stride(0)
+
+    def _plain(self, t, name, dtype, n):
+        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == dtype and t.is_contiguous() and t.numel() == n):
+            raise TypeError(f"{name}: expected a contiguous tensor on {self.device} of dtype {dtype} with {n} elements")
+        return t.data_ptr()
+
+    def _out_rows(self, out, dtype, x, rows, n):
+        """The result [x's rows, n] (a vector where x is one), its pointer and its stride."""
+        if out is None:
+            out = self._new((n,) if x.dim() == 1 else (rows, n), dtype)
+            return out, out.data_ptr(), n
+        got, ld = self._rows_of(out, "out", (dtype,), n)
+        if got != rows or out.dim() != x.dim():
+            raise TypeError(f"out: expected {rows} rows of {n} elements, like x, got shape {tuple(out.shape)}")
+        return out, out.data_ptr(), ld
+
+    @staticmethod
+    def grouped_bytes(rows, cols, group):
+        out = C.c_size_t()
+        _chk(lib().skim_grouped_bytes(rows, cols, group, C.byref(out)), "skim_grouped_bytes")
+        return out.value
+
+    def _tiles(self, q, name):
+        t, rows, cols, group = q["tiles"], q["rows"], q["cols"], q["group"]
+        if not (t.device == self.device and t.dtype == torch.uint8 and t.is_contiguous()):
+            raise TypeError(f"{name}: expected contiguous uint8 tiles on {self.device}")
+        if group not in (32, 64, 128) or t.numel() < -(-rows // 16) * -(-cols // 128) * (1024 + 8192 // group):
+            raise TypeError(f"{name}: {t.numel()} bytes of tiles do not hold {rows} x {cols} weights in groups of {group}")
+        return t.data_ptr(), rows, cols, group
+
+    def grouped_quantize(self, W, group=128, importance=None, want_err=False, out=None):
+        """Uniform 4-bit codes with a scale and a zero point per ``group`` (32, 64 or 128) columns of the float16 matrix W (of W / alpha
+        where a scale vector is installed).  Returns dict(tiles uint8, rows, cols, group, err): the stored form, which grouped_dequantize, grouped_matvec
+        and grouped_gated read, and (want_err) the float32 [rows] error, weighted with ``importance`` (float32, like W), else None."""
+        rows, ld = self._rows_of(W, "W", (torch.float16,))
+        cols = W.shape[-1]
+        if W.dim() != 2:
+            raise TypeError(f"W: expected a matrix, got shape {tuple(W.shape)}")
+        if importance is not None:
+            got, ldg = self._rows_of(importance, "importance", (torch.float32,), cols)
+            if got != rows or ldg != ld:
+                raise TypeError("importance: expected the shape and the strides of W")
+        if out is None:
+            out = dict(tiles=self._new((self.grouped_bytes(rows, cols, group),), torch.uint8), rows=rows, cols=cols, group=group,
+                       err=self._new((rows,), torch.float32) if want_err else None)
+        tiles, *held = self._tiles(out, "out")
+        if held != [rows, cols, group]:
+            raise TypeError(f"out: holds rows, cols, group {held}, expected {[rows, cols, group]}")
+        err = out.get("err")
+        _chk(lib().skim_grouped_quantize(self._h, W.data_ptr(), None if importance is None else importance.data_ptr(), rows, cols, ld, group, tiles,
+                                         None if err is None else self._plain(err, "err", torch.float32, rows)), "skim_grouped_quantize")
+        return out
+
+    def grouped_dequantize(self, q, out=None):
+        """float16 [rows, cols] values of a grouped_quantize() result."""
+        tiles, rows, cols, group = self._tiles(q, "q")
+        if out is None:
+            out = self._new((rows, cols), torch.float16)
+        got, ld = self._rows_of(out, "out", (torch.float16,), cols)
+        if got != rows:
+            raise TypeError(f"out: expected {rows} rows, got {got}")
+        _chk(lib().skim_grouped_dequantize(self._h, tiles, rows, cols, group, out.data_ptr(), ld), "skim_grouped_dequantize")
+        return out
+
+    def _tokens(self, x, x_scale, cols):
+        tokens, ldx = self._rows_of(x, "x", (torch.float16, torch.bfloat16, torch.int8), cols)
+        return tokens, ldx, TYPES[x.dtype], None if x_scale is None else self._plain(x_scale, "x_scale", torch.float32, tokens)
+
+    def grouped_matvec(self, q, x, x_scale=None, out=None, out_dtype=torch.float32):
+        """[tokens, rows] (or [rows] for a vector x): x_scale * x Wq^T for float16, bfloat16 or int8 rows x [tokens, cols], straight from a
+        grouped_quantize() result ``q``; out_dtype is float32, float16 or bfloat16."""
+        tiles, rows, cols, group = self._tiles(q, "q")
+        tokens, ldx, kind, scale = self._tokens(x, x_scale, cols)
+        out, y, ldy = self._out_rows(out, out_dtype if out is None else out.dtype, x, tokens, rows)
+        _chk(lib().skim_grouped_matvec(self._h, tiles, rows, cols, group, x.data_ptr(), kind, ldx, scale, tokens, y, TYPES.get(out.dtype, -1), ldy),
+             "skim_grouped_matvec")
+        return out
+
+    def grouped_gated(self, gate, up, x, x_scale=None, activation="silu", out=None, out_dtype=torch.float32):
+        """act(gate x) * (up x) for two grouped_quantize() results of one shape; arguments as for grouped_matvec, activation "silu" or "gelu"."""
+        tiles, rows, cols, group = self._tiles(gate, "gate")
+        other, *held = self._tiles(up, "up")
+        if held != [rows, cols, group]:
+            raise TypeError(f"up: holds rows, cols, group {held}, gate {[rows, cols, group]}")
+        tokens, ldx, kind, scale = self._tokens(x, x_scale, cols)
+        out, y, ldy = self._out_rows(out, out_dtype if out is None else out.dtype, x, tokens, rows)
+        _chk(lib().skim_grouped_gated(self._h, tiles, other, rows, cols, group, ACTIVATIONS.get(activation, -1), x.data_ptr(), kind, ldx, scale,
+                                      tokens, y, TYPES.get(out.dtype, -1), ldy), "skim_grouped_gated")
+        return out
+
+    def add_rmsnorm(self, x, weight=None, eps=1e-5, residual=None, out_dtype=None, out=None, out_scale=None, sum_out=None):
+        """The root-mean-square norm of x + residual, times ``weight`` [cols].  Returns (out, out_scale, sum): out in x's dtype (float16 or
+        bfloat16) with out_scale None, or, out_dtype torch.int8, codes with out_scale float32 [rows]; sum is x + residual, the new residual stream, or
+        None without a residual (unless sum_out is given).  sum_out may be residual or x itself."""
+        dtypes = (torch.float16, torch.bfloat16)
+        rows, ldx = self._rows_of(x, "x", dtypes)
+        cols, kind = x.shape[-1], x.dtype
+        out, y, ldo = self._out_rows(out, (out_dtype or kind) if out is None else out.dtype, x, rows, cols)
+        ldr = lds = 0
+        if residual is not None:
+            got, ldr = self._rows_of(residual, "residual", (kind,), cols)
+            if got != rows:
+                raise TypeError(f"residual: expected {rows} rows, got {got}")
+            if sum_out is None:
+                sum_out = self._new(x.shape, kind)
+        if sum_out is not None:
+            got, lds = self._rows_of(sum_out, "sum_out", (kind,), cols)
+            if got != rows:
+                raise TypeError(f"sum_out: expected {rows} rows, got {got}")
+        if out.dtype == torch.int8 and out_scale is None:
+            out_scale = self._new((rows,), torch.float32)
+        _chk(lib().skim_add_rmsnorm(self._h, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
+                                    None if weight is None else self._plain(weight, "weight", kind, cols), TYPES[kind], rows, cols, eps,
+                                    None if sum_out is None else sum_out.data_ptr(), lds, y, TYPES.get(out.dtype, -1), ldo,
+                                    None if out_scale is None else self._plain(out_scale, "out_scale", torch.float32, rows)), "skim_add_rmsnorm")
+        return out, out_scale, sum_out
+
+    def feed_forward(self, x, weight, gate, up, down, eps=1e-5, residual=None, activation="silu", eight_bit=True, out=None):
+        """The feed-forward half of a decoder layer: add_rmsnorm (to 8 bits, or to x's dtype), grouped_gated, grouped_matvec.  Returns (down's
+        product in x's dtype, the new residual stream or None); ``gate`` and ``up`` are [hidden, cols], ``down`` [cols, hidden]."""
+        rows, scale, stream = self.add_rmsnorm(x, weight, eps=eps, residual=residual, out_dtype=torch.int8 if eight_bit else None)
+        hidden = self.grouped_gated(gate, up, rows, x_scale=scale, activation=activation, out_dtype=x.dtype)
+        return self.grouped_matvec(down, hidden, out=out, out_dtype=x.dtype), stream
 
     def scale_update(self, W, importance, labels, alpha, steps=120, lr0=0.01, decay=0.5, decay_every=40,
                      want_trace=True):
