@@ -300,7 +300,7 @@ int skim_matvec(skim_ctx *ctx, const uint32_t *packed, const int32_t *row_order,
 #define SKIM_ACT_SILU 0           /* g / (1 + exp(-g)) */
 #define SKIM_ACT_GELU 1           /* 0.5 g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) */
 #define SKIM_MAX_TOKENS 1048560   /* token rows of one call */
-#define SKIM_MAX_GROUPED_COLS 16777216
+#define SKIM_MAX_GROUPED_COLS 131072
 
 /*
  * Uniform 4-bit quantisation with group scales: the form the paper's codebooks are compared with (the baselines of its

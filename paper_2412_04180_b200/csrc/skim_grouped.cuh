@@ -36,32 +36,40 @@ struct Zero<false> {
     __half2 near, far;           // 1024 + z, -(64 + z)
     __device__ __forceinline__ explicit Zero(uint32_t meta)
     {
-        near = bits_half2(__byte_perm(meta, 0u, 0x4242) | 0x64006400u);
+        near = bits_half2(__byte_perm(meta, 0x64u, 0x4242));
         far = __hsub2(bits_half2(0x63806380u), near);                    // 960 - (1024 + z)
     }
 };
 template <>
 struct Zero<true> {
     __nv_bfloat162 near;         // 128 + z
-    __device__ __forceinline__ explicit Zero(uint32_t meta) { near = bits_bf162(__byte_perm(meta, 0u, 0x4242) | 0x43004300u); }
+    __device__ __forceinline__ explicit Zero(uint32_t meta) { near = bits_bf162(__byte_perm(meta, 0x43u, 0x4242)); }
 };
 __device__ __forceinline__ float meta_scale(uint32_t meta) { return __half2float(__ushort_as_half((unsigned short)(meta & 0xffffu))); }
+
+// (a & mask) | with, one operation
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t with)
+{
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(a), "r"(mask), "r"(with));
+    return r;
+}
 
 // code - z of a word's eight columns, as pairs of neighbours.  A nibble ORed into the low bits of 1024 (the bfloat16 128) is that number plus the code,
 // exactly; the second nibble of a byte comes out sixteenfold and is scaled back in the subtraction.  All results are whole and exact.
 __device__ __forceinline__ void expand(uint32_t w, const Zero<false> &z, uint32_t out[4])
 {
     const __half2 sixteenth = bits_half2(0x2c002c00u);
-    out[0] = half2_bits(__hsub2(bits_half2((w & 0x000f000fu) | 0x64006400u), z.near));
-    out[1] = half2_bits(__hfma2(bits_half2((w & 0x00f000f0u) | 0x64006400u), sixteenth, z.far));
+    out[0] = half2_bits(__hsub2(bits_half2(and_or(w, 0x000f000fu, 0x64006400u)), z.near));
+    out[1] = half2_bits(__hfma2(bits_half2(and_or(w, 0x00f000f0u, 0x64006400u)), sixteenth, z.far));
     w >>= 8;
-    out[2] = half2_bits(__hsub2(bits_half2((w & 0x000f000fu) | 0x64006400u), z.near));
-    out[3] = half2_bits(__hfma2(bits_half2((w & 0x00f000f0u) | 0x64006400u), sixteenth, z.far));
+    out[2] = half2_bits(__hsub2(bits_half2(and_or(w, 0x000f000fu, 0x64006400u)), z.near));
+    out[3] = half2_bits(__hfma2(bits_half2(and_or(w, 0x00f000f0u, 0x64006400u)), sixteenth, z.far));
 }
 __device__ __forceinline__ void expand(uint32_t w, const Zero<true> &z, uint32_t out[4])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = bf162_bits(__hsub2(bits_bf162(((w >> (4 * i)) & 0x000f000fu) | 0x43004300u), z.near));
+    for (int i = 0; i < 4; ++i) out[i] = bf162_bits(__hsub2(bits_bf162(and_or(w >> (4 * i), 0x000f000fu, 0x43004300u)), z.near));
 }
 
 // Eight 8-bit activations as pairs of binary16 numbers: b + 128 ORed into the low bits of 1024, less 1152.

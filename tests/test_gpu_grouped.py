@@ -259,7 +259,7 @@ def test_what_is_not_finite_stays_in_its_row(ctx, tokens, dtype):
 
 def test_few_rows_and_long_rows_share_the_columns(ctx):
     """Few rows: blocks of a cluster share the columns.  8-bit rows without a scale and whole weights give whole sums below 2^24: no rounding anywhere."""
-    for rows, cols, tokens in [(16, 4096, 1), (5, 16384, 8), (33, 22016, 3), (16, 9000, 16), (16, 8200, 33), (128, 8192, 70)]:
+    for rows, cols, tokens in [(16, 4096, 1), (5, 16384, 8), (33, 22016, 3), (16, 9000, 16), (16, 8200, 33), (128, 8192, 70), (20, 131072, 17)]:
         rng = np.random.default_rng(cols)
         w = rng.integers(-1, 15, (rows, cols))
         w[:, 0::32] = -1

@@ -87,7 +87,7 @@ def test_grouped_bytes(lib):
     assert Skim.grouped_bytes(16, 128, 128) == 1088 and Skim.grouped_bytes(17, 129, 64) == 4 * 1152 and Skim.grouped_bytes(1, 1, 32) == 1280
     n = C.c_size_t()
     assert lib.skim_grouped_bytes(1, 1, 32, None) == NULL
-    for rows, cols, group, code in [(-1, 1, 32, SHAPE), (1, 0, 32, SHAPE), (1, 16777217, 32, SHAPE), (1 << 31, 1, 32, SHAPE), (1, 1, 16, TYPE), (1, 1, 256, TYPE)]:
+    for rows, cols, group, code in [(-1, 1, 32, SHAPE), (1, 0, 32, SHAPE), (1, 131073, 32, SHAPE), (1 << 31, 1, 32, SHAPE), (1, 1, 16, TYPE), (1, 1, 256, TYPE)]:
         assert lib.skim_grouped_bytes(rows, cols, group, C.byref(n)) == code
 
 
@@ -116,7 +116,7 @@ def test_product_refusals(lib, handle):
     both(WORKSPACE)
     for bad in (dict(ctx=None), dict(tiles=None), dict(x=None), dict(y=None)):
         both(NULL, **bad)
-    for bad in (dict(rows=-1), dict(cols=0), dict(cols=16777217, ldx=1 << 30), dict(ldx=63), dict(ldy=3), dict(tokens=-1), dict(tokens=1048561)):
+    for bad in (dict(rows=-1), dict(cols=0), dict(cols=131073, ldx=1 << 30), dict(ldx=63), dict(ldy=3), dict(tokens=-1), dict(tokens=1048561)):
         both(SHAPE, **bad)
     for bad in (dict(group=0), dict(group=96), dict(xt=2), dict(xt=4), dict(xt=-1), dict(yt=3), dict(yt=-1)):
         both(TYPE, **bad)
