@@ -709,7 +709,8 @@ int grouped_product(skim_ctx *ctx, const SkimGroupedProduct &p)
     if (!guard.ok) return SKIM_ERR_CUDA;
     SkimGroupedProduct q = p;
     q.status = (unsigned long long *)ctx->ws;
-    return skim_launch_grouped_small(ctx, q);
+    if (none) return SKIM_OK;
+    return skim_grouped_gemm_takes(q) ? skim_launch_grouped_gemm(ctx, q) : skim_launch_grouped_small(ctx, q);
 }
 
 }  // namespace

@@ -168,6 +168,8 @@ struct SkimGroupedProduct {
     int64_t ldo;
     unsigned long long *status;
 };
+bool skim_grouped_gemm_takes(const SkimGroupedProduct &p);
+int skim_launch_grouped_gemm(skim_ctx *ctx, const SkimGroupedProduct &p);
 int skim_launch_grouped_small(skim_ctx *ctx, const SkimGroupedProduct &p);
 int skim_launch_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *importance, const float *rscale, int64_t rows, int64_t cols, int64_t ld, int group,
                                  unsigned char *tiles, float *err);

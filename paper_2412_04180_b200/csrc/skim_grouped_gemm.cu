@@ -1,0 +1,506 @@
+// Products of many token rows with matrices in the stored form of skim_grouped.cuh, on the fifth-generation tensor cores:
+//
+//   y[t][i] = sum over groups of s_ig * sum_{j in the group} (q_ij - z_ig) x[t][j],   gated: act(gate product) * (up product)
+//
+// Bound by the tensor pipe.  A pair of CTAs has a tile of 256 weight rows (128 each) and two accumulators of up to 128 tokens in tensor memory: two runs of
+// tokens, or the gate's and the up's rows with the same tokens.  The weights are operand A, and never touch shared memory: four warps expand a record's codes,
+// less their zero points, in registers and store them to tensor memory (exact binary16 or bfloat16 numbers), from where tcgen05.mma reads them.  The tokens
+// are operand B, brought by TMA, half of them by each CTA.  The values are not rounded to 16 bits: an accumulator holds one group's sum, in binary32, and eight warps
+// take it times the group's scale into binary32 totals in their registers, while the tensor cores are at the other accumulator.
+// (A tile of its own for every CTA would ask the L2 for 64 bytes a clock and SM for the tokens alone; the pair asks for half of that.)
+// Where tiles are few the pairs of a cluster share the columns and add their totals, in a fixed order, through shared memory.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include "skim_grouped.cuh"
+
+namespace {
+
+using namespace skimg;
+
+constexpr int CM = 128, BM = 2 * CM;             // weight rows of a CTA, of a pair
+constexpr int BK = SKIM_RECORD_COLS;             // columns of a step: one record
+constexpr int RECS = CM / SKIM_RECORD_ROWS;      // records of a CTA's rows in a step
+constexpr int EXPAND_WARPS = 4, SUM_WARPS = 8, THREADS = (EXPAND_WARPS + SUM_WARPS + 4) * 32;
+constexpr int WARP_TMA = EXPAND_WARPS + SUM_WARPS, WARP_MMA = WARP_TMA + 1, WARP_CODES = WARP_TMA + 2;
+constexpr int MAX_SPLIT = 4;
+
+// What tensor memory and shared memory hold.  A group's sum goes the round of product, signal, readback and signal in some 1500 clocks while its products take 512
+// (128 tokens, group of 128), so three accumulators are under way; a tile of operand A goes its round of expansion and product faster.
+template <int PER, bool GATED>
+struct Shape {
+    static constexpr int N = GATED ? 96 : 128;                           // tokens of an accumulator, at most
+    static constexpr int MATS = GATED ? 2 : 1;
+    static constexpr int D_PLACES = 3, A_PLACES = GATED ? 3 : 2, A_COLS = BK / 2, A_COL = D_PLACES * N, TMEM_COLS = 512;
+    static_assert(A_COL + A_PLACES * A_COLS <= TMEM_COLS, "tensor memory");
+    static constexpr int BOX = N / 2 * 128;                              // this CTA's tokens of an accumulator, 64 columns
+    static constexpr int B_PLACES = 5, B_BYTES = (GATED ? 1 : 2) * 2 * BOX;
+    static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, C_PLACES = GATED ? 3 : 5, C_BYTES = MATS * RECS * RECORD;
+    static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? CM * N * 4 : 0), SYNC_BYTES = 512;
+    static constexpr size_t SMEM = 1024 + SYNC_AT + SYNC_BYTES;
+    static_assert(SMEM <= 227 * 1024 && N * SUM_WARPS * 32 * 4 <= SYNC_AT, "shared memory; the totals of a split tile fit");
+};
+
+struct GemmArgs {
+    SkimGroupedProduct p;
+    int ct;
+    int64_t rt;              // rows of records
+    int mt, nt;              // tiles along weight rows, along tokens
+    int nh;                  // tokens of an accumulator (a multiple of 32, which products with operand A in tensor memory ask for)
+    int split;               // pairs of a cluster: they share the columns
+};
+
+struct Sync {
+    uint64_t b_full[5], b_empty[5];
+    uint64_t a_full[3], a_empty[3];
+    uint64_t c_full[5], c_empty[5];
+    uint64_t d_full[3], d_empty[3];
+    uint32_t tmem;
+    int abort;               // a wait ran out
+};
+static_assert(sizeof(Sync) <= 512, "the barriers' part of the shared memory");
+
+__device__ __forceinline__ uint32_t address_in(const void *p, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_address(p)), "r"(rank));
+    return r;
+}
+// What is handed over lies in tensor memory and is ordered by tcgen05's fences: no release beyond the block, whose fence would cost hundreds of clocks a time.
+__device__ __forceinline__ void arrive_at(uint32_t addr) { asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory"); }
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Sync &sy)
+{
+    if (barrier_try(bar, parity)) return true;
+    const long long t0 = clock64();
+    while (!barrier_try(bar, parity)) {
+        if (*(volatile int *)&sy.abort) return false;
+        if (clock64() - t0 > WAIT_CYCLES) {
+            *(volatile int *)&sy.abort = 1;
+            return false;
+        }
+    }
+    return true;
+}
+// By a whole warp, whose lanes go on together.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Sync &sy) { return __all_sync(0xffffffffu, wait_for(bar, parity, sy)) != 0; }
+// 64 columns of some token rows into this CTA's shared memory; the bytes are counted at `bar`, in the pair's first CTA.
+__device__ __forceinline__ void tma_tokens(void *dst, const CUtensorMap *map, uint32_t bar, int col, int token)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(smem_address(dst)),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(col), "r"(token)
+                 : "memory");
+}
+// Operand B in shared memory: rows of 64 16-bit numbers = 128 bytes, 128-byte swizzle, groups of 8 rows 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand_b(uint32_t addr)
+{
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+// kind::f16, binary32 accumulators, A and B both binary16 or both bfloat16, K-major, 256 rows, n columns.
+__device__ __forceinline__ uint32_t instruction_of(bool bf16, int n) { return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(BM >> 4) << 24; }
+__device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint64_t b, uint32_t instruction, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(instruction),
+                 "r"(accumulate)
+                 : "memory");
+}
+// Arrives at this offset in both CTAs of the pair once the products issued so far are done.
+__device__ __forceinline__ void commit_to(uint64_t *bar, uint16_t both)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_address(bar)), "h"(both) : "memory");
+}
+__device__ __forceinline__ bool elect_lane()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// 16 consecutive 32-bit columns of this thread's lane of tensor memory; wait_loads() before the values are used.
+__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t *v)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(at));
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t *v)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+                 : "memory");
+}
+
+template <int N>
+__device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N>
+__device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+// A block is launched with 128 registers a thread; of the four warpgroups one takes 104, two 176, one 40: 496 of 512.
+__device__ __forceinline__ void sums_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(SUM_WARPS * 32) : "memory"); }
+
+template <bool BF16, int PER, bool GATED>
+__global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __grid_constant__ CUtensorMap tokens_map, GemmArgs a)
+{
+    using S = Shape<PER, GATED>;
+    constexpr int STEPS = BK / 16 / PER;                     // instructions of a group
+    extern __shared__ unsigned char raw[];
+    unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023), *code_ring = ring + S::CODES_AT;
+    Sync &sy = *reinterpret_cast<Sync *>(ring + S::SYNC_AT);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank_of_block(), leader = rank & ~1u, mine = rank & 1u;
+    const int part = (int)(rank >> 1), clusters = (int)gridDim.x / (2 * a.split), first = (int)blockIdx.x / (2 * a.split);
+    const int k0 = a.ct * part / a.split, k1 = a.ct * (part + 1) / a.split, tiles = a.mt * a.nt;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::B_PLACES; ++s) { barrier_init(&sy.b_full[s], 1); barrier_init(&sy.b_empty[s], 1); }
+        for (int s = 0; s < S::A_PLACES; ++s) { barrier_init(&sy.a_full[s], 2 * EXPAND_WARPS); barrier_init(&sy.a_empty[s], 1); }
+        for (int s = 0; s < S::C_PLACES; ++s) { barrier_init(&sy.c_full[s], 1); barrier_init(&sy.c_empty[s], EXPAND_WARPS); }
+        for (int s = 0; s < S::D_PLACES; ++s) { barrier_init(&sy.d_full[s], 1); barrier_init(&sy.d_empty[s], SUM_WARPS); }
+        sy.abort = 0;
+        barrier_init_fence();
+    }
+    if (warp == WARP_MMA) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_address(&sy.tmem)), "r"(S::TMEM_COLS));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    }
+    fence_before();
+    __syncthreads();
+    cluster_barrier();
+    fence_after();
+    skim_wait_for_previous_kernel();
+    skim_let_next_kernel_start();
+    const uint32_t tmem = sy.tmem;
+    bool ok = true;
+
+    if (warp < EXPAND_WARPS) {
+        // ---------------------------------------------------------------- codes to operand A; a thread has a row
+        fewer_registers<104>();
+        int place = 0, from = 0, step = 0;
+        uint32_t phase = 0, phase_c = 0;
+        const int in = warp * 32 + lane;
+        const uint32_t to = tmem + ((uint32_t)(warp * 32) << 16) + S::A_COL;
+        for (int t = first; t < tiles && ok; t += clusters) {
+            for (int c = k0; c < k1 && ok; ++c) {
+                if (!(ok = warp_wait(&sy.c_full[from], phase_c, sy))) break;
+#pragma unroll
+                for (int m = 0; m < S::MATS; ++m) {
+                    const unsigned char *r = code_ring + from * S::C_BYTES + (m * RECS + in / SKIM_RECORD_ROWS) * S::RECORD;
+                    uint4 codes[4];
+                    uint32_t meta[PER];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) codes[p] = *reinterpret_cast<const uint4 *>(r + (in % SKIM_RECORD_ROWS) * 64 + p * 16);
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) meta[k] = reinterpret_cast<const uint32_t *>(r + SKIM_RECORD_CODES)[in % SKIM_RECORD_ROWS * PER + k];
+                    if (m == S::MATS - 1) {
+                        __syncwarp();
+                        if (lane == 0) barrier_arrive(&sy.c_empty[from]);
+                    }
+                    // one matrix: the place is free when the step A_PLACES before is done, which frees its tokens' place too, with one arrival for both
+                    if (GATED) ok = ok && warp_wait(&sy.a_empty[place], phase ^ 1u, sy);
+                    else if (step >= S::A_PLACES) ok = warp_wait(&sy.b_empty[(step - S::A_PLACES) % S::B_PLACES], (uint32_t)((step - S::A_PLACES) / S::B_PLACES) & 1u, sy);
+                    if (!ok) break;
+                    fence_after();
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t out[32];
+#pragma unroll
+                        for (int t2 = 0; t2 < 2; ++t2) {
+                            const int tt = 2 * h + t2;
+                            const Zero<BF16> z(meta[tt * PER / 4]);
+#pragma unroll
+                            for (int p = 0; p < 4; ++p) expand(tt == 0 ? codes[p].x : tt == 1 ? codes[p].y : tt == 2 ? codes[p].z : codes[p].w, z, out + 16 * t2 + 4 * p);
+                        }
+                        tmem_store32(to + place * S::A_COLS + 32 * h, out);
+                    }
+                    wait_stores();
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_at(address_in(&sy.a_full[place], leader));
+                    if (++place == S::A_PLACES) { place = 0; phase ^= 1u; }
+                }
+                if (++from == S::C_PLACES) { from = 0; phase_c ^= 1u; }
+                ++step;
+            }
+        }
+    } else if (warp < EXPAND_WARPS + SUM_WARPS) {
+        // ---------------------------------------------------------------- groups' sums times their scales; a thread has a row of one accumulator
+        more_registers<176>();
+        const int quarter = warp & 3, j = (warp - EXPAND_WARPS) >> 2;
+        int unit = GATED ? j * PER : j;                      // of the accumulators in the order of the products
+        const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
+        const unsigned char *matrix = a.p.tiles[GATED ? j : 0];
+        // (every warp goes through all tiles even where a wait ran out: they meet at barriers)
+        for (int t = first; t < tiles; t += clusters) {
+            const int64_t row = (int64_t)(t % a.mt) * BM + mine * CM + quarter * 32 + lane, rec = row / SKIM_RECORD_ROWS;
+            const bool live = rec < a.rt;
+            const unsigned char *at = matrix + (live ? (rec * a.ct + k0) * S::RECORD + SKIM_RECORD_CODES + (row % SKIM_RECORD_ROWS) * (4 * PER) : 0);
+            uint32_t meta[PER];
+            float total[S::N];
+#pragma unroll
+            for (int i = 0; i < S::N; ++i) total[i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < PER; ++k) meta[k] = __ldg(reinterpret_cast<const uint32_t *>(at) + k);
+            for (int c = k0; c < k1 && ok; ++c) {
+                float scale[PER];
+#pragma unroll
+                for (int k = 0; k < PER; ++k) scale[k] = meta_scale(meta[k]);
+                if (c + 1 < k1) {
+                    if (live) at += S::RECORD;
+#pragma unroll
+                    for (int k = 0; k < PER; ++k) meta[k] = __ldg(reinterpret_cast<const uint32_t *>(at) + k);
+                }
+#pragma unroll
+                for (int k = 0; k < PER; ++k) {
+                    const int place = unit % S::D_PLACES;
+                    // a barrier tells only the last phase from the one before it: where the other matrix' groups came between, the place's last use is seen first
+                    if (GATED && PER > 2 && k == 0 && ok && unit >= S::D_PLACES) ok = warp_wait(&sy.d_full[place], (uint32_t)(unit / S::D_PLACES - 1) & 1u, sy);
+                    if (!ok || !(ok = warp_wait(&sy.d_full[place], (uint32_t)(unit / S::D_PLACES) & 1u, sy))) break;
+                    fence_after();
+                    const float s = scale[k];
+                    uint32_t v[2][16];
+                    tmem_load16(from + place * S::N, v[0]);
+#pragma unroll
+                    for (int i = 0; i < S::N; i += 16) {
+                        if (i >= a.nh) break;
+                        wait_loads();
+                        if (i + 16 < S::N && i + 16 < a.nh) {
+                            tmem_load16(from + place * S::N + i + 16, v[(i / 16 + 1) & 1]);
+                        } else {
+                            fence_before();
+                            __syncwarp();
+                            if (lane == 0) arrive_at(address_in(&sy.d_empty[place], leader));
+                        }
+#pragma unroll
+                        for (int u = 0; u < 16; ++u) total[i + u] = fmaf(s, __uint_as_float(v[(i / 16) & 1][u]), total[i + u]);
+                    }
+                    unit += GATED ? (k == PER - 1 ? PER + 1 : 1) : 2;
+                }
+            }
+            if (a.split > 1) {
+                // the pairs of the cluster have one tile; the rings are no longer used: totals go there, [token][thread]
+                float *all = reinterpret_cast<float *>(ring);
+#pragma unroll
+                for (int i = 0; i < S::N; ++i)
+                    if (i < a.nh) all[i * (SUM_WARPS * 32) + (int)threadIdx.x - EXPAND_WARPS * 32] = total[i];
+            } else if (GATED) {
+                // the two halves of the tokens are finished by the gate's and the up's warps, which give one another the other half
+                float *swap = reinterpret_cast<float *>(ring + S::SWAP_AT);
+                const int r = quarter * 32 + lane, h0 = j * (S::N / 2);
+#pragma unroll
+                for (int i = 0; i < S::N / 2; ++i) swap[(S::N / 2 - h0 + i) * CM + r] = j ? total[i] : total[S::N / 2 + i];
+                sums_barrier();
+                const int64_t t0 = (int64_t)(t / a.mt) * a.nh + h0;
+#pragma unroll
+                for (int i = 0; i < S::N / 2; ++i) {
+                    const float other = swap[(h0 + i) * CM + r], own = j ? total[S::N / 2 + i] : total[i];
+                    if (ok && row < a.p.rows && h0 + i < a.nh && t0 + i < a.p.tokens)
+                        store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, activation(a.p.act, j ? other : own) * (j ? own : other));
+                }
+                sums_barrier();
+            } else if (ok && row < a.p.rows) {
+                const int64_t t0 = (int64_t)(t / a.mt) * (2 * a.nh) + j * a.nh;
+#pragma unroll
+                for (int i = 0; i < S::N; ++i)
+                    if (i < a.nh && t0 + i < a.p.tokens) store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, total[i]);
+            }
+        }
+    } else {
+        fewer_registers<40>();
+        if (warp == WARP_TMA && lane == 0) {
+            // ------------------------------------------------------------ tokens
+            const uint32_t bytes = (uint32_t)(GATED ? 1 : 2) * 2 * (a.nh / 2) * 128;
+            int place = 0, issued = 0;
+            uint32_t phase = 0;
+            for (int t = first; t < tiles && ok; t += clusters) {
+                const int t0 = (t / a.mt) * (GATED ? a.nh : 2 * a.nh) + (int)mine * (a.nh / 2);
+                for (int c = k0; c < k1; ++c) {
+                    if (!(ok = wait_for(&sy.b_empty[place], phase ^ 1u, sy))) break;
+                    unsigned char *to = ring + (size_t)place * S::B_BYTES;
+                    if (mine == 0) barrier_expect(&sy.b_full[place], 2 * bytes);
+                    const uint32_t bar = address_in(&sy.b_full[place], leader);
+                    for (int j = 0; j < (GATED ? 1 : 2); ++j)
+                        for (int h = 0; h < 2; ++h) tma_tokens(to + (j * 2 + h) * S::BOX, &tokens_map, bar, c * BK + h * 64, t0 + j * a.nh);
+                    ++issued;
+                    if (++place == S::B_PLACES) { place = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok && mine == 0)                              // copies on their way land before the block ends
+                for (int i = issued > S::B_PLACES ? issued - S::B_PLACES : 0; i < issued; ++i) barrier_wait(&sy.b_full[i % S::B_PLACES], (uint32_t)(i / S::B_PLACES) & 1u, WAIT_CYCLES / 16);
+        } else if (warp == WARP_CODES) {
+            // ------------------------------------------------------------ records: a lane has one of each matrix' eight
+            int place = 0, issued = 0;
+            uint32_t phase = 0;
+            for (int t = first; t < tiles && ok; t += clusters) {
+                const int64_t rec = ((int64_t)(t % a.mt) * BM + mine * CM) / SKIM_RECORD_ROWS + (lane & (RECS - 1));
+                const bool live = lane < S::MATS * RECS && rec < a.rt;
+                const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, live)) * S::RECORD;
+                const unsigned char *src = a.p.tiles[lane < RECS ? 0 : S::MATS - 1] + (rec * a.ct + k0) * S::RECORD;
+                for (int c = k0; c < k1; ++c, src += S::RECORD) {
+                    if (!(ok = warp_wait(&sy.c_empty[place], phase ^ 1u, sy))) break;
+                    if (lane == 0) barrier_expect(&sy.c_full[place], bytes);
+                    __syncwarp();
+                    if (live) bulk_copy(code_ring + place * S::C_BYTES + lane * S::RECORD, src, S::RECORD, &sy.c_full[place]);
+                    ++issued;
+                    if (++place == S::C_PLACES) { place = 0; phase ^= 1u; }
+                }
+            }
+            if (!ok)
+                for (int i = issued > S::C_PLACES ? issued - S::C_PLACES : 0; i < issued; ++i) barrier_wait(&sy.c_full[i % S::C_PLACES], (uint32_t)(i / S::C_PLACES) & 1u, WAIT_CYCLES / 16);
+        } else if (warp == WARP_MMA && mine == 0) {
+            // ------------------------------------------------------------ products, for both CTAs.  The whole warp goes through the loops, so that operands are
+            // warp-uniform values, and one lane issues (one lane's own loops: 61 clocks an instruction and 750 a group)
+            const uint32_t instruction = instruction_of(BF16, a.nh);
+            const uint16_t both = (uint16_t)(3u << leader);
+            const bool issues = elect_lane();
+            int pa = 0, pb = 0, pd = 0;
+            uint32_t phase_a = 0, phase_b = 0, phase_d = 1;
+            // one group of one accumulator: tile of A at a_at, tokens j, group k
+            auto group = [&](uint32_t a_at, uint64_t b, int k) {
+                if (!ok || !(ok = warp_wait(&sy.d_empty[pd], phase_d, sy))) return;
+                fence_after();
+                const uint32_t d = tmem + pd * S::N;
+                if (issues) {
+#pragma unroll
+                    for (int u = 0; u < STEPS; ++u) {
+                        const int step = k * STEPS + u;
+                        multiply(d, a_at + step * 8, b + (((step >> 2) * S::BOX + (step & 3) * 32) >> 4), instruction, u > 0);
+                    }
+                    commit_to(&sy.d_full[pd], both);
+                }
+                __syncwarp();
+                if (++pd == S::D_PLACES) { pd = 0; phase_d ^= 1u; }
+            };
+            for (int t = first; t < tiles && ok; t += clusters)
+                for (int c = k0; c < k1 && ok; ++c) {
+                    if (!(ok = warp_wait(&sy.b_full[pb], phase_b, sy))) break;
+                    const uint64_t b = operand_b(smem_address(ring + (size_t)pb * S::B_BYTES));
+#pragma unroll
+                    for (int m = 0; m < S::MATS; ++m) {
+                        if (!ok || !(ok = warp_wait(&sy.a_full[pa], phase_a, sy))) break;
+                        fence_after();
+                        const uint32_t a_at = tmem + S::A_COL + pa * S::A_COLS;
+#pragma unroll
+                        for (int k = 0; k < PER; ++k) {
+                            group(a_at, b, k);
+                            if (!GATED) group(a_at, b + (2 * S::BOX >> 4), k);
+                        }
+                        if (GATED && issues) commit_to(&sy.a_empty[pa], both);
+                        __syncwarp();
+                        if (++pa == S::A_PLACES) { pa = 0; phase_a ^= 1u; }
+                    }
+                    if (issues) commit_to(&sy.b_empty[pb], both);
+                    __syncwarp();
+                    if (++pb == S::B_PLACES) { pb = 0; phase_b ^= 1u; }
+                }
+        }
+    }
+    __syncthreads();
+    if (sy.abort) {
+        for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // copies and products in flight end before the block does
+        if (threadIdx.x == 0) atomicOr(a.p.status, (unsigned long long)SKIM_STATUS_TIMEOUT);
+    }
+    fence_before();
+    cluster_barrier();
+    if (a.split > 1) {
+        // every pair's totals lie in shared memory, in order of rank; a pair finishes the tokens i with i % split == its number
+        const int r = (int)threadIdx.x & (CM - 1), slice = (int)threadIdx.x / CM;
+        const int64_t row = (int64_t)(first % a.mt) * BM + mine * CM + r, t0 = (int64_t)(first / a.mt) * (GATED ? a.nh : 2 * a.nh);
+        const float *all = reinterpret_cast<const float *>(ring) + r;
+        auto sum_of = [&](int i, int j) {
+            float s = 0.0f;
+            for (int p = 0; p < a.split; ++p) s += load_from_rank(all + i * (SUM_WARPS * 32) + j * CM, 2 * p + mine);
+            return s;
+        };
+        if (row < a.p.rows)
+            for (int i = part + a.split * slice; i < a.nh; i += a.split * (THREADS / CM)) {
+                if (GATED) {
+                    if (t0 + i < a.p.tokens) store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, activation(a.p.act, sum_of(i, 0)) * sum_of(i, 1));
+                } else {
+                    for (int j = 0; j < 2; ++j)
+                        if (t0 + j * a.nh + i < a.p.tokens) store_as(a.p.out, a.p.out_type, (t0 + j * a.nh + i) * a.p.ldo + row, sum_of(i, j));
+                }
+            }
+        cluster_barrier();                                     // read before the others end
+    }
+    if (warp == WARP_MMA) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM_COLS));
+    }
+}
+
+int encode_tokens(CUtensorMap *map, const SkimGroupedProduct &p, int box_rows)
+{
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) return SKIM_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)p.cols, (cuuint64_t)p.tokens}, strides[1] = {(cuuint64_t)p.ldx * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    const CUresult r = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn)(
+        map, p.x_type == SKIM_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(p.x), dims, strides, box, steps,
+        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? SKIM_OK : SKIM_ERR_CUDA;
+}
+
+template <bool BF16, int PER, bool GATED>
+int launch(skim_ctx *ctx, const CUtensorMap &map, const GemmArgs &a)
+{
+    auto kernel = skim_grouped_gemm_kernel<BF16, PER, GATED>;
+    constexpr size_t SMEM = Shape<PER, GATED>::SMEM;
+    SKIM_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM));
+    const int pairs = ctx->sm_count / 2, tiles = a.mt * a.nt;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (a.split > 1 ? tiles * a.split : tiles < pairs ? tiles : pairs)));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = SMEM;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)(2 * a.split);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    SKIM_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, map, a));
+    ctx->launches += 1;
+    return SKIM_OK;
+}
+template <bool BF16, bool GATED>
+int launch_by_group(skim_ctx *ctx, const CUtensorMap &map, const GemmArgs &a)
+{
+    switch (a.p.group) {
+    case 128: return launch<BF16, 1, GATED>(ctx, map, a);
+    case 64: return launch<BF16, 2, GATED>(ctx, map, a);
+    default: return launch<BF16, 4, GATED>(ctx, map, a);
+    }
+}
+
+}  // namespace
+
+bool skim_grouped_gemm_takes(const SkimGroupedProduct &p)
+{
+    if (p.x_type == SKIM_TYPE_I8 || p.x_scale) return false;
+    if ((reinterpret_cast<uintptr_t>(p.x) & 15u) || p.ldx % 8 || p.tokens > 0x3fffffff || p.rows > 0x3fffffff) return false;
+    return p.tokens > 64;
+}
+
+int skim_launch_grouped_gemm(skim_ctx *ctx, const SkimGroupedProduct &p)
+{
+    GemmArgs a;
+    a.p = p;
+    a.ct = (int)skim_record_tiles(p.cols, SKIM_RECORD_COLS);
+    a.rt = skim_record_tiles(p.rows, SKIM_RECORD_ROWS);
+    a.mt = (int)skim_record_tiles(p.rows, BM);
+    const int most = p.gated ? Shape<1, true>::N : 2 * Shape<1, false>::N;
+    a.nt = (int)skim_record_tiles(p.tokens, most);
+    const int64_t each = skim_record_tiles(p.tokens, a.nt);
+    a.nh = (int)skim_record_tiles(p.gated ? each : (each + 1) / 2, 32) * 32;
+    if ((int64_t)a.mt * a.nt > 0x1fffffff) return SKIM_ERR_SHAPE;
+    a.split = 1;
+    const int pairs = ctx->sm_count / 2;
+    while (a.split < MAX_SPLIT && (int64_t)a.mt * a.nt * a.split * 2 <= pairs && a.ct >= a.split * 4) a.split *= 2;
+    CUtensorMap map;
+    const int rc = encode_tokens(&map, p, a.nh / 2);
+    if (rc) return rc;
+    if (p.x_type == SKIM_TYPE_BF16) return p.gated ? launch_by_group<true, true>(ctx, map, a) : launch_by_group<true, false>(ctx, map, a);
+    return p.gated ? launch_by_group<false, true>(ctx, map, a) : launch_by_group<false, false>(ctx, map, a);
+}
