@@ -36,7 +36,7 @@ struct Shape {
     static constexpr int BOX = N / 2 * 128;                              // this CTA's tokens of an accumulator, 64 columns
     static constexpr int B_PLACES = 5, B_BYTES = (GATED ? 1 : 2) * 2 * BOX;
     static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, C_PLACES = GATED ? 3 : 5, C_BYTES = MATS * RECS * RECORD;
-    static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? CM * N * 4 : 0), SYNC_BYTES = 512;
+    static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? 2 * CM * N * 4 : 0), SYNC_BYTES = 512;
     static constexpr size_t SMEM = 1024 + SYNC_AT + SYNC_BYTES;
     static_assert(SMEM <= 227 * 1024 && N * SUM_WARPS * 32 * 4 <= SYNC_AT, "shared memory; the totals of a split tile fit");
 };
@@ -116,13 +116,12 @@ __device__ __forceinline__ bool elect_lane()
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void wait_loads() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// 16 consecutive 32-bit columns of this thread's lane of tensor memory; wait_loads() before the values are used.
-__device__ __forceinline__ void tmem_load16(uint32_t at, uint32_t *v)
+// 32 consecutive 32-bit columns of this thread's lane of tensor memory; wait_loads() before the values are used, which it names, so that no use moves in front of it.
+__device__ __forceinline__ void tmem_load32(uint32_t at, uint32_t *v)
 {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]), "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]), "=r"(v[31])
                  : "r"(at));
 }
 __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t *v)
@@ -130,13 +129,32 @@ __device__ __forceinline__ void tmem_store32(uint32_t at, const uint32_t *v)
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(at), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
                  : "memory");
 }
+__device__ __forceinline__ void wait_loads(uint32_t *v)
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
+}
 
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// A block is launched with 128 registers a thread; of the four warpgroups one takes 104, two 176, one 40: 496 of 512.
+// A block is launched with 128 registers a thread; of the four warpgroups one takes 72, two 208, one 24.
 __device__ __forceinline__ void sums_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(SUM_WARPS * 32) : "memory"); }
+
+__device__ __forceinline__ void store_one(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store_one(__half *p, float v) { *p = __float2half_rn(v); }
+__device__ __forceinline__ void store_one(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
+// The first n tokens of a row: few instructions for each, since they are many.
+template <int N, typename Out>
+__device__ __forceinline__ void store_totals(Out *p, int64_t stride, int n, const float *total)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if (i < n) store_one(p, total[i]);
+        p += stride;
+    }
+}
 
 template <bool BF16, int PER, bool GATED>
 __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __grid_constant__ CUtensorMap tokens_map, GemmArgs a)
@@ -173,7 +191,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
 
     if (warp < EXPAND_WARPS) {
         // ---------------------------------------------------------------- codes to operand A; a thread has a row
-        fewer_registers<104>();
+        fewer_registers<72>();
         int place = 0, from = 0, step = 0;
         uint32_t phase = 0, phase_c = 0;
         const int in = warp * 32 + lane;
@@ -223,7 +241,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
         }
     } else if (warp < EXPAND_WARPS + SUM_WARPS) {
         // ---------------------------------------------------------------- groups' sums times their scales; a thread has a row of one accumulator
-        more_registers<176>();
+        more_registers<208>();
         const int quarter = warp & 3, j = (warp - EXPAND_WARPS) >> 2;
         int unit = GATED ? j * PER : j;                      // of the accumulators in the order of the products
         const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
@@ -256,21 +274,21 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                     if (!ok || !(ok = warp_wait(&sy.d_full[place], (uint32_t)(unit / S::D_PLACES) & 1u, sy))) break;
                     fence_after();
                     const float s = scale[k];
-                    uint32_t v[2][16];
-                    tmem_load16(from + place * S::N, v[0]);
+                    uint32_t v[2][32];
+                    tmem_load32(from + place * S::N, v[0]);
 #pragma unroll
-                    for (int i = 0; i < S::N; i += 16) {
+                    for (int i = 0; i < S::N; i += 32) {
                         if (i >= a.nh) break;
-                        wait_loads();
-                        if (i + 16 < S::N && i + 16 < a.nh) {
-                            tmem_load16(from + place * S::N + i + 16, v[(i / 16 + 1) & 1]);
+                        wait_loads(v[(i / 32) & 1]);
+                        if (i + 32 < S::N && i + 32 < a.nh) {
+                            tmem_load32(from + place * S::N + i + 32, v[(i / 32 + 1) & 1]);
                         } else {
                             fence_before();
                             __syncwarp();
                             if (lane == 0) arrive_at(address_in(&sy.d_empty[place], leader));
                         }
 #pragma unroll
-                        for (int u = 0; u < 16; ++u) total[i + u] = fmaf(s, __uint_as_float(v[(i / 16) & 1][u]), total[i + u]);
+                        for (int u = 0; u < 32; ++u) total[i + u] = fmaf(s, __uint_as_float(v[(i / 32) & 1][u]), total[i + u]);
                     }
                     unit += GATED ? (k == PER - 1 ? PER + 1 : 1) : 2;
                 }
@@ -282,29 +300,28 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                 for (int i = 0; i < S::N; ++i)
                     if (i < a.nh) all[i * (SUM_WARPS * 32) + (int)threadIdx.x - EXPAND_WARPS * 32] = total[i];
             } else if (GATED) {
-                // the two halves of the tokens are finished by the gate's and the up's warps, which give one another the other half
-                float *swap = reinterpret_cast<float *>(ring + S::SWAP_AT);
-                const int r = quarter * 32 + lane, h0 = j * (S::N / 2);
+                // gate and up meet in shared memory; the gate's warps finish one half of the tokens, the up's the other.  (A loop: unrolled, with its registers, this
+                // code did not fit the instruction cache and took 27 000 clocks a tile.)
+                float *swap = reinterpret_cast<float *>(ring + S::SWAP_AT) + quarter * 32 + lane;
 #pragma unroll
-                for (int i = 0; i < S::N / 2; ++i) swap[(S::N / 2 - h0 + i) * CM + r] = j ? total[i] : total[S::N / 2 + i];
+                for (int i = 0; i < S::N; ++i) swap[(j * S::N + i) * CM] = total[i];
                 sums_barrier();
-                const int64_t t0 = (int64_t)(t / a.mt) * a.nh + h0;
-#pragma unroll
-                for (int i = 0; i < S::N / 2; ++i) {
-                    const float other = swap[(h0 + i) * CM + r], own = j ? total[S::N / 2 + i] : total[i];
-                    if (ok && row < a.p.rows && h0 + i < a.nh && t0 + i < a.p.tokens)
-                        store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, activation(a.p.act, j ? other : own) * (j ? own : other));
-                }
+                const int64_t t0 = (int64_t)(t / a.mt) * a.nh;
+                if (ok && row < a.p.rows)
+#pragma unroll 1
+                    for (int i = j * (a.nh / 2); i < (j + 1) * (a.nh / 2) && t0 + i < a.p.tokens; ++i)
+                        store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, activation(a.p.act, swap[i * CM]) * swap[(S::N + i) * CM]);
                 sums_barrier();
             } else if (ok && row < a.p.rows) {
                 const int64_t t0 = (int64_t)(t / a.mt) * (2 * a.nh) + j * a.nh;
-#pragma unroll
-                for (int i = 0; i < S::N; ++i)
-                    if (i < a.nh && t0 + i < a.p.tokens) store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, total[i]);
+                const int n = (int)(a.p.tokens - t0 < a.nh ? a.p.tokens - t0 : a.nh);
+                if (a.p.out_type == SKIM_TYPE_F32) store_totals<S::N>(static_cast<float *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, n, total);
+                else if (a.p.out_type == SKIM_TYPE_F16) store_totals<S::N>(static_cast<__half *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, n, total);
+                else store_totals<S::N>(static_cast<__nv_bfloat16 *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, n, total);
             }
         }
     } else {
-        fewer_registers<40>();
+        fewer_registers<24>();
         if (warp == WARP_TMA && lane == 0) {
             // ------------------------------------------------------------ tokens
             const uint32_t bytes = (uint32_t)(GATED ? 1 : 2) * 2 * (a.nh / 2) * 128;
