@@ -29,14 +29,14 @@ constexpr int MAX_SPLIT = 4;
 // (128 tokens, group of 128), so three accumulators are under way; a tile of operand A goes its round of expansion and product faster.
 template <int PER, bool GATED>
 struct Shape {
-    static constexpr int N = GATED ? 96 : 128;                           // tokens of an accumulator, at most
+    static constexpr int N = 128;                                        // tokens of an accumulator, at most
     static constexpr int MATS = GATED ? 2 : 1;
-    static constexpr int D_PLACES = 3, A_PLACES = GATED ? 3 : 2, A_COLS = BK / 2, A_COL = D_PLACES * N, TMEM_COLS = 512;
+    static constexpr int D_PLACES = 3, A_PLACES = 2, A_COLS = BK / 2, A_COL = D_PLACES * N, TMEM_COLS = 512;
     static_assert(A_COL + A_PLACES * A_COLS <= TMEM_COLS, "tensor memory");
     static constexpr int BOX = N / 2 * 128;                              // this CTA's tokens of an accumulator, 64 columns
     static constexpr int B_PLACES = 5, B_BYTES = (GATED ? 1 : 2) * 2 * BOX;
     static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, C_PLACES = GATED ? 3 : 5, C_BYTES = MATS * RECS * RECORD;
-    static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? 2 * CM * N * 4 : 0), SYNC_BYTES = 512;
+    static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? CM * N * 4 : 0), SYNC_BYTES = 512;
     static constexpr size_t SMEM = 1024 + SYNC_AT + SYNC_BYTES;
     static_assert(SMEM <= 227 * 1024 && N * SUM_WARPS * 32 * 4 <= SYNC_AT, "shared memory; the totals of a split tile fit");
 };
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
         const unsigned char *matrix = a.p.tiles[GATED ? j : 0];
         // (every warp goes through all tiles even where a wait ran out: they meet at barriers)
         for (int t = first; t < tiles; t += clusters) {
-            const int64_t row = (int64_t)(t % a.mt) * BM + mine * CM + quarter * 32 + lane, rec = row / SKIM_RECORD_ROWS;
+            const int64_t row = (int64_t)(t / a.nt) * BM + mine * CM + quarter * 32 + lane, rec = row / SKIM_RECORD_ROWS;
             const bool live = rec < a.rt;
             const unsigned char *at = matrix + (live ? (rec * a.ct + k0) * S::RECORD + SKIM_RECORD_CODES + (row % SKIM_RECORD_ROWS) * (4 * PER) : 0);
             uint32_t meta[PER];
@@ -300,20 +300,24 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                 for (int i = 0; i < S::N; ++i)
                     if (i < a.nh) all[i * (SUM_WARPS * 32) + (int)threadIdx.x - EXPAND_WARPS * 32] = total[i];
             } else if (GATED) {
-                // gate and up meet in shared memory; the gate's warps finish one half of the tokens, the up's the other.  (A loop: unrolled, with its registers, this
+                // gate and up meet in shared memory, one half of the tokens after the other; the gate's warps finish one half of that, the up's the other.  (A loop: unrolled, with its registers, this
                 // code did not fit the instruction cache and took 27 000 clocks a tile.)
                 float *swap = reinterpret_cast<float *>(ring + S::SWAP_AT) + quarter * 32 + lane;
+                const int64_t t0 = (int64_t)(t % a.nt) * a.nh;
 #pragma unroll
-                for (int i = 0; i < S::N; ++i) swap[(j * S::N + i) * CM] = total[i];
-                sums_barrier();
-                const int64_t t0 = (int64_t)(t / a.mt) * a.nh;
-                if (ok && row < a.p.rows)
+                for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                    for (int i = 0; i < S::N / 2; ++i) swap[(j * (S::N / 2) + i) * CM] = total[h * (S::N / 2) + i];
+                    sums_barrier();
+                    const int first_i = j * (S::N / 4), end = (int)(a.p.tokens - t0 - h * (S::N / 2) < first_i + S::N / 4 ? a.p.tokens - t0 - h * (S::N / 2) : first_i + S::N / 4);
+                    if (ok && row < a.p.rows)
 #pragma unroll 1
-                    for (int i = j * (a.nh / 2); i < (j + 1) * (a.nh / 2) && t0 + i < a.p.tokens; ++i)
-                        store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, activation(a.p.act, swap[i * CM]) * swap[(S::N + i) * CM]);
-                sums_barrier();
+                        for (int i = first_i; i < end && h * (S::N / 2) + i < a.nh; ++i)
+                            store_as(a.p.out, a.p.out_type, (t0 + h * (S::N / 2) + i) * a.p.ldo + row, activation(a.p.act, swap[i * CM]) * swap[(S::N / 2 + i) * CM]);
+                    sums_barrier();
+                }
             } else if (ok && row < a.p.rows) {
-                const int64_t t0 = (int64_t)(t / a.mt) * (2 * a.nh) + j * a.nh;
+                const int64_t t0 = (int64_t)(t % a.nt) * (2 * a.nh) + j * a.nh;
                 const int n = (int)(a.p.tokens - t0 < a.nh ? a.p.tokens - t0 : a.nh);
                 if (a.p.out_type == SKIM_TYPE_F32) store_totals<S::N>(static_cast<float *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, n, total);
                 else if (a.p.out_type == SKIM_TYPE_F16) store_totals<S::N>(static_cast<__half *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, n, total);
@@ -328,7 +332,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
             int place = 0, issued = 0;
             uint32_t phase = 0;
             for (int t = first; t < tiles && ok; t += clusters) {
-                const int t0 = (t / a.mt) * (GATED ? a.nh : 2 * a.nh) + (int)mine * (a.nh / 2);
+                const int t0 = (t % a.nt) * (GATED ? a.nh : 2 * a.nh) + (int)mine * (a.nh / 2);
                 for (int c = k0; c < k1; ++c) {
                     if (!(ok = wait_for(&sy.b_empty[place], phase ^ 1u, sy))) break;
                     unsigned char *to = ring + (size_t)place * S::B_BYTES;
@@ -347,7 +351,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
             int place = 0, issued = 0;
             uint32_t phase = 0;
             for (int t = first; t < tiles && ok; t += clusters) {
-                const int64_t rec = ((int64_t)(t % a.mt) * BM + mine * CM) / SKIM_RECORD_ROWS + (lane & (RECS - 1));
+                const int64_t rec = ((int64_t)(t / a.nt) * BM + mine * CM) / SKIM_RECORD_ROWS + (lane & (RECS - 1));
                 const bool live = lane < S::MATS * RECS && rec < a.rt;
                 const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, live)) * S::RECORD;
                 const unsigned char *src = a.p.tiles[lane < RECS ? 0 : S::MATS - 1] + (rec * a.ct + k0) * S::RECORD;
@@ -410,6 +414,9 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                 }
         }
     }
+    // what follows is every warp's, and compiled for the registers of the launch
+    if (warp >= EXPAND_WARPS && warp < EXPAND_WARPS + SUM_WARPS) fewer_registers<128>();
+    else more_registers<128>();
     __syncthreads();
     if (sy.abort) {
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // copies and products in flight end before the block does
@@ -420,7 +427,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
     if (a.split > 1) {
         // every pair's totals lie in shared memory, in order of rank; a pair finishes the tokens i with i % split == its number
         const int r = (int)threadIdx.x & (CM - 1), slice = (int)threadIdx.x / CM;
-        const int64_t row = (int64_t)(first % a.mt) * BM + mine * CM + r, t0 = (int64_t)(first / a.mt) * (GATED ? a.nh : 2 * a.nh);
+        const int64_t row = (int64_t)(first / a.nt) * BM + mine * CM + r, t0 = (int64_t)(first % a.nt) * (GATED ? a.nh : 2 * a.nh);
         const float *all = reinterpret_cast<const float *>(ring) + r;
         auto sum_of = [&](int i, int j) {
             float s = 0.0f;
