@@ -130,6 +130,8 @@ __device__ __forceinline__ void bulk_copy(void *dst, const void *src, uint32_t b
                  "r"(smem_address(bar))
                  : "memory");
 }
+// Between a thread's last read of a place in shared memory and what lets a bulk copy overwrite it.
+__device__ __forceinline__ void read_before_copy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void cluster_barrier()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");

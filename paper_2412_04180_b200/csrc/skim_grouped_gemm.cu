@@ -2,12 +2,12 @@
 //
 //   y[t][i] = sum over groups of s_ig * sum_{j in the group} (q_ij - z_ig) x[t][j],   gated: act(gate product) * (up product)
 //
-// Bound by the tensor pipe.  A pair of CTAs has a tile of 256 weight rows (128 each) and two accumulators of up to 128 tokens in tensor memory: two runs of
-// tokens, or the gate's and the up's rows with the same tokens.  The weights are operand A, and never touch shared memory: four warps expand a record's codes,
-// less their zero points, in registers and store them to tensor memory (exact binary16 or bfloat16 numbers), from where tcgen05.mma reads them.  The tokens
-// are operand B, brought by TMA, half of them by each CTA.  The values are not rounded to 16 bits: an accumulator holds one group's sum, in binary32, and eight warps
-// take it times the group's scale into binary32 totals in their registers, while the tensor cores are at the other accumulator.
-// (A tile of its own for every CTA would ask the L2 for 64 bytes a clock and SM for the tokens alone; the pair asks for half of that.)
+// Bound by the tensor pipe and by the round of signals about it.  A pair of CTAs has a tile of 256 weight rows, 128 each (gated: 64 of the gate and the same 64 of
+// the up matrix), times up to 192 tokens.  The weights are operand A, and never touch shared memory as numbers: four warps expand a record's codes, less
+// their zero points, in registers and store them to tensor memory (exact binary16 or bfloat16 numbers), from where tcgen05.mma reads them.  The tokens are operand
+// B, brought by TMA, half of them by each CTA: a tile of its own for every CTA would ask the L2 for twice the bytes.  The values are not rounded to 16 bits: an
+// accumulator holds one group's sum, in binary32, and eight warps take it times the group's scale into binary32 totals in their registers,
+// while the tensor cores are at the next one.
 // Where tiles are few the pairs of a cluster share the columns and add their totals, in a fixed order, through shared memory.
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -25,20 +25,20 @@ constexpr int EXPAND_WARPS = 4, SUM_WARPS = 8, THREADS = (EXPAND_WARPS + SUM_WAR
 constexpr int WARP_TMA = EXPAND_WARPS + SUM_WARPS, WARP_MMA = WARP_TMA + 1, WARP_CODES = WARP_TMA + 2;
 constexpr int MAX_SPLIT = 4;
 
-// What tensor memory and shared memory hold.  A group's sum goes the round of product, signal, readback and signal in some 1500 clocks while its products take 512
-// (128 tokens, group of 128), so three accumulators are under way; a tile of operand A goes its round of expansion and product faster.
+// What tensor memory and shared memory hold.  A group's sum goes a round of product, signal, readback and signal; issuing a group's products and signals
+// takes one warp some 700 clocks however long they are.  So with groups of 128 the accumulators are wide (192 tokens: 768 clocks of products) and two; with
+// smaller groups, where the round counts, narrower and three.
 template <int PER, bool GATED>
 struct Shape {
-    static constexpr int N = 128;                                        // tokens of an accumulator, at most
-    static constexpr int MATS = GATED ? 2 : 1;
-    static constexpr int D_PLACES = 3, A_PLACES = 2, A_COLS = BK / 2, A_COL = D_PLACES * N, TMEM_COLS = 512;
+    static constexpr int N = PER == 1 ? 192 : 128, D_PLACES = PER == 1 ? 2 : 3;      // tokens of an accumulator, at most; accumulators
+    static constexpr int A_PLACES = 2, A_COLS = BK / 2, A_COL = D_PLACES * N, TMEM_COLS = 512;
     static_assert(A_COL + A_PLACES * A_COLS <= TMEM_COLS, "tensor memory");
-    static constexpr int BOX = N / 2 * 128;                              // this CTA's tokens of an accumulator, 64 columns
-    static constexpr int B_PLACES = 5, B_BYTES = (GATED ? 1 : 2) * 2 * BOX;
-    static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, C_PLACES = GATED ? 3 : 5, C_BYTES = MATS * RECS * RECORD;
-    static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? CM * N * 4 : 0), SYNC_BYTES = 512;
+    static constexpr int BOX = N / 2 * 128;                              // this CTA's tokens, 64 columns
+    static constexpr int B_PLACES = PER == 1 && GATED ? 4 : 5, B_BYTES = 2 * BOX;
+    static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, C_PLACES = 5, C_BYTES = RECS * RECORD;
+    static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? CM * N / 2 * 4 : 0), SYNC_BYTES = 512;
     static constexpr size_t SMEM = 1024 + SYNC_AT + SYNC_BYTES;
-    static_assert(SMEM <= 227 * 1024 && N * SUM_WARPS * 32 * 4 <= SYNC_AT, "shared memory; the totals of a split tile fit");
+    static_assert(SMEM <= 227 * 1024 && N * CM * 4 <= SYNC_AT, "shared memory; the totals of a split tile fit");
 };
 
 struct GemmArgs {
@@ -46,15 +46,15 @@ struct GemmArgs {
     int ct;
     int64_t rt;              // rows of records
     int mt, nt;              // tiles along weight rows, along tokens
-    int nh;                  // tokens of an accumulator (a multiple of 32, which products with operand A in tensor memory ask for)
+    int n;                   // tokens of a tile (a multiple of 32, which products with operand A in tensor memory ask for)
     int split;               // pairs of a cluster: they share the columns
 };
 
 struct Sync {
-    uint64_t b_full[5], b_empty[5];
-    uint64_t a_full[3], a_empty[3];
-    uint64_t c_full[5], c_empty[5];
-    uint64_t d_full[3], d_empty[3];
+    uint64_t b_full[5], b_empty[5];      // a step's tokens; b_empty: its products are done, which frees its operand A too
+    uint64_t a_full[2];
+    uint64_t c_full[5], c_empty[5];      // records
+    uint64_t d_full[3], d_empty[3];      // accumulators
     uint32_t tmem;
     int abort;               // a wait ran out
 };
@@ -134,14 +134,12 @@ __device__ __forceinline__ void wait_loads(uint32_t *v)
     asm volatile("tcgen05.wait::ld.sync.aligned;"
                  : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]), "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15]), "+r"(v[16]), "+r"(v[17]), "+r"(v[18]), "+r"(v[19]), "+r"(v[20]), "+r"(v[21]), "+r"(v[22]), "+r"(v[23]), "+r"(v[24]), "+r"(v[25]), "+r"(v[26]), "+r"(v[27]), "+r"(v[28]), "+r"(v[29]), "+r"(v[30]), "+r"(v[31])::"memory");
 }
-
 template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// A block is launched with 128 registers a thread; of the four warpgroups one takes 72, two 208, one 24.
+// A block is launched with 128 registers a thread; of the four warpgroups one takes 104, two 176, one 40.
 __device__ __forceinline__ void sums_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(SUM_WARPS * 32) : "memory"); }
-
 __device__ __forceinline__ void store_one(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_one(__half *p, float v) { *p = __float2half_rn(v); }
 __device__ __forceinline__ void store_one(__nv_bfloat16 *p, float v) { *p = __float2bfloat16_rn(v); }
@@ -155,6 +153,12 @@ __device__ __forceinline__ void store_totals(Out *p, int64_t stride, int n, cons
         p += stride;
     }
 }
+
+// Row of the matrix, and the matrix, that row r of this CTA's tile m is.
+template <bool GATED>
+__device__ __forceinline__ int64_t row_of(int m, uint32_t mine, int r) { return GATED ? (int64_t)m * CM + mine * (CM / 2) + (r & (CM / 2 - 1)) : (int64_t)m * BM + mine * CM + r; }
+template <bool GATED>
+__device__ __forceinline__ int matrix_of(int r) { return GATED && r >= CM / 2 ? 1 : 0; }
 
 template <bool BF16, int PER, bool GATED>
 __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __grid_constant__ CUtensorMap tokens_map, GemmArgs a)
@@ -170,9 +174,9 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
     const int k0 = a.ct * part / a.split, k1 = a.ct * (part + 1) / a.split, tiles = a.mt * a.nt;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S::B_PLACES; ++s) { barrier_init(&sy.b_full[s], 1); barrier_init(&sy.b_empty[s], 1); }
-        for (int s = 0; s < S::A_PLACES; ++s) { barrier_init(&sy.a_full[s], 2 * EXPAND_WARPS); barrier_init(&sy.a_empty[s], 1); }
+        for (int s = 0; s < S::A_PLACES; ++s) barrier_init(&sy.a_full[s], 2 * EXPAND_WARPS);
         for (int s = 0; s < S::C_PLACES; ++s) { barrier_init(&sy.c_full[s], 1); barrier_init(&sy.c_empty[s], EXPAND_WARPS); }
-        for (int s = 0; s < S::D_PLACES; ++s) { barrier_init(&sy.d_full[s], 1); barrier_init(&sy.d_empty[s], SUM_WARPS); }
+        for (int s = 0; s < S::D_PLACES; ++s) { barrier_init(&sy.d_full[s], 1); barrier_init(&sy.d_empty[s], 2 * SUM_WARPS); }
         sy.abort = 0;
         barrier_init_fence();
     }
@@ -186,75 +190,70 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
     fence_after();
     skim_wait_for_previous_kernel();
     skim_let_next_kernel_start();
-    const uint32_t tmem = sy.tmem;
-    bool ok = true;
+    const uint32_t tmem = 0u;                                // all columns are this block's, so they begin at 0: a constant keeps the operands warp-uniform
+    bool ok = sy.tmem == 0u;
+    if (!ok) *(volatile int *)&sy.abort = 1;
 
     if (warp < EXPAND_WARPS) {
         // ---------------------------------------------------------------- codes to operand A; a thread has a row
-        fewer_registers<72>();
-        int place = 0, from = 0, step = 0;
-        uint32_t phase = 0, phase_c = 0;
+        fewer_registers<104>();
+        int from = 0, step = 0;
+        uint32_t phase_c = 0;
         const int in = warp * 32 + lane;
         const uint32_t to = tmem + ((uint32_t)(warp * 32) << 16) + S::A_COL;
-        for (int t = first; t < tiles && ok; t += clusters) {
-            for (int c = k0; c < k1 && ok; ++c) {
+        for (int t = first; t < tiles && ok; t += clusters)
+            for (int c = k0; c < k1; ++c, ++step) {
                 if (!(ok = warp_wait(&sy.c_full[from], phase_c, sy))) break;
+                const unsigned char *r = code_ring + from * S::C_BYTES + in / SKIM_RECORD_ROWS * S::RECORD;
+                uint4 codes[4];
+                uint32_t meta[PER];
 #pragma unroll
-                for (int m = 0; m < S::MATS; ++m) {
-                    const unsigned char *r = code_ring + from * S::C_BYTES + (m * RECS + in / SKIM_RECORD_ROWS) * S::RECORD;
-                    uint4 codes[4];
-                    uint32_t meta[PER];
+                for (int p = 0; p < 4; ++p) codes[p] = *reinterpret_cast<const uint4 *>(r + (in % SKIM_RECORD_ROWS) * 64 + p * 16);
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) codes[p] = *reinterpret_cast<const uint4 *>(r + (in % SKIM_RECORD_ROWS) * 64 + p * 16);
+                for (int k = 0; k < PER; ++k) meta[k] = reinterpret_cast<const uint32_t *>(r + SKIM_RECORD_CODES)[in % SKIM_RECORD_ROWS * PER + k];
+                const int place = step % S::A_PLACES, before = step - S::A_PLACES;          // the place is free when the step that had it is done
+                if (before >= 0 && !(ok = warp_wait(&sy.b_empty[before % S::B_PLACES], (uint32_t)(before / S::B_PLACES) & 1u, sy))) break;
+                fence_after();
 #pragma unroll
-                    for (int k = 0; k < PER; ++k) meta[k] = reinterpret_cast<const uint32_t *>(r + SKIM_RECORD_CODES)[in % SKIM_RECORD_ROWS * PER + k];
-                    if (m == S::MATS - 1) {
-                        __syncwarp();
-                        if (lane == 0) barrier_arrive(&sy.c_empty[from]);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t out[32];
+#pragma unroll
+                    for (int t2 = 0; t2 < 2; ++t2) {
+                        const int tt = 2 * h + t2;
+                        const Zero<BF16> z(meta[tt * PER / 4]);
+#pragma unroll
+                        for (int p = 0; p < 4; ++p) expand(tt == 0 ? codes[p].x : tt == 1 ? codes[p].y : tt == 2 ? codes[p].z : codes[p].w, z, out + 16 * t2 + 4 * p);
                     }
-                    // one matrix: the place is free when the step A_PLACES before is done, which frees its tokens' place too, with one arrival for both
-                    if (GATED) ok = ok && warp_wait(&sy.a_empty[place], phase ^ 1u, sy);
-                    else if (step >= S::A_PLACES) ok = warp_wait(&sy.b_empty[(step - S::A_PLACES) % S::B_PLACES], (uint32_t)((step - S::A_PLACES) / S::B_PLACES) & 1u, sy);
-                    if (!ok) break;
-                    fence_after();
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t out[32];
-#pragma unroll
-                        for (int t2 = 0; t2 < 2; ++t2) {
-                            const int tt = 2 * h + t2;
-                            const Zero<BF16> z(meta[tt * PER / 4]);
-#pragma unroll
-                            for (int p = 0; p < 4; ++p) expand(tt == 0 ? codes[p].x : tt == 1 ? codes[p].y : tt == 2 ? codes[p].z : codes[p].w, z, out + 16 * t2 + 4 * p);
-                        }
-                        tmem_store32(to + place * S::A_COLS + 32 * h, out);
-                    }
-                    wait_stores();
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) arrive_at(address_in(&sy.a_full[place], leader));
-                    if (++place == S::A_PLACES) { place = 0; phase ^= 1u; }
+                    tmem_store32(to + place * S::A_COLS + 32 * h, out);
+                }
+                wait_stores();
+                fence_before();
+                read_before_copy();                          // (given back before the values' last use, a place was overwritten before it was read)
+                __syncwarp();
+                if (lane == 0) {
+                    arrive_at(address_in(&sy.a_full[place], leader));
+                    barrier_arrive(&sy.c_empty[from]);
                 }
                 if (++from == S::C_PLACES) { from = 0; phase_c ^= 1u; }
-                ++step;
             }
-        }
     } else if (warp < EXPAND_WARPS + SUM_WARPS) {
-        // ---------------------------------------------------------------- groups' sums times their scales; a thread has a row of one accumulator
-        more_registers<208>();
-        const int quarter = warp & 3, j = (warp - EXPAND_WARPS) >> 2;
-        int unit = GATED ? j * PER : j;                      // of the accumulators in the order of the products
-        const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16);
-        const unsigned char *matrix = a.p.tiles[GATED ? j : 0];
+        // ---------------------------------------------------------------- groups' sums times their scales; a thread has a row and half of the tokens
+        more_registers<176>();
+        constexpr int H = S::N / 2;
+        const int quarter = warp & 3, half = (warp - EXPAND_WARPS) >> 2, r = quarter * 32 + lane, h = a.n / 2;
+        int place = 0;
+        uint32_t phase = 0;
+        const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + half * h;
+        const unsigned char *matrix = a.p.tiles[matrix_of<GATED>(r)];
         // (every warp goes through all tiles even where a wait ran out: they meet at barriers)
         for (int t = first; t < tiles; t += clusters) {
-            const int64_t row = (int64_t)(t / a.nt) * BM + mine * CM + quarter * 32 + lane, rec = row / SKIM_RECORD_ROWS;
+            const int64_t row = row_of<GATED>(t / a.nt, mine, r), rec = row / SKIM_RECORD_ROWS;
             const bool live = rec < a.rt;
             const unsigned char *at = matrix + (live ? (rec * a.ct + k0) * S::RECORD + SKIM_RECORD_CODES + (row % SKIM_RECORD_ROWS) * (4 * PER) : 0);
             uint32_t meta[PER];
-            float total[S::N];
+            float total[H];
 #pragma unroll
-            for (int i = 0; i < S::N; ++i) total[i] = 0.0f;
+            for (int i = 0; i < H; ++i) total[i] = 0.0f;
 #pragma unroll
             for (int k = 0; k < PER; ++k) meta[k] = __ldg(reinterpret_cast<const uint32_t *>(at) + k);
             for (int c = k0; c < k1 && ok; ++c) {
@@ -268,19 +267,16 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                 }
 #pragma unroll
                 for (int k = 0; k < PER; ++k) {
-                    const int place = unit % S::D_PLACES;
-                    // a barrier tells only the last phase from the one before it: where the other matrix' groups came between, the place's last use is seen first
-                    if (GATED && PER > 2 && k == 0 && ok && unit >= S::D_PLACES) ok = warp_wait(&sy.d_full[place], (uint32_t)(unit / S::D_PLACES - 1) & 1u, sy);
-                    if (!ok || !(ok = warp_wait(&sy.d_full[place], (uint32_t)(unit / S::D_PLACES) & 1u, sy))) break;
+                    if (!ok || !(ok = warp_wait(&sy.d_full[place], phase, sy))) break;
                     fence_after();
                     const float s = scale[k];
                     uint32_t v[2][32];
                     tmem_load32(from + place * S::N, v[0]);
 #pragma unroll
-                    for (int i = 0; i < S::N; i += 32) {
-                        if (i >= a.nh) break;
+                    for (int i = 0; i < H; i += 32) {
+                        if (i >= h) break;                   // (h is a multiple of 16: the last read may take 16 columns of the other half along, unused)
                         wait_loads(v[(i / 32) & 1]);
-                        if (i + 32 < S::N && i + 32 < a.nh) {
+                        if (i + 32 < H && i + 32 < h) {
                             tmem_load32(from + place * S::N + i + 32, v[(i / 32 + 1) & 1]);
                         } else {
                             fence_before();
@@ -290,56 +286,55 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
 #pragma unroll
                         for (int u = 0; u < 32; ++u) total[i + u] = fmaf(s, __uint_as_float(v[(i / 32) & 1][u]), total[i + u]);
                     }
-                    unit += GATED ? (k == PER - 1 ? PER + 1 : 1) : 2;
+                    if (++place == S::D_PLACES) { place = 0; phase ^= 1u; }
                 }
             }
+            const int64_t t0 = (int64_t)(t % a.nt) * a.n + half * h;
+            const int left = (int)(a.p.tokens - t0 < h ? a.p.tokens - t0 : h);             // this thread's tokens (none: below 1)
             if (a.split > 1) {
-                // the pairs of the cluster have one tile; the rings are no longer used: totals go there, [token][thread]
-                float *all = reinterpret_cast<float *>(ring);
+                // the pairs of the cluster have one tile; the rings are no longer used: totals go there, [token][row]
+                float *all = reinterpret_cast<float *>(ring) + half * h * CM + r;
 #pragma unroll
-                for (int i = 0; i < S::N; ++i)
-                    if (i < a.nh) all[i * (SUM_WARPS * 32) + (int)threadIdx.x - EXPAND_WARPS * 32] = total[i];
+                for (int i = 0; i < H; ++i)
+                    if (i < h) all[i * CM] = total[i];
             } else if (GATED) {
-                // gate and up meet in shared memory, one half of the tokens after the other; the gate's warps finish one half of that, the up's the other.  (A loop: unrolled, with its registers, this
-                // code did not fit the instruction cache and took 27 000 clocks a tile.)
-                float *swap = reinterpret_cast<float *>(ring + S::SWAP_AT) + quarter * 32 + lane;
-                const int64_t t0 = (int64_t)(t % a.nt) * a.nh;
+                // Gate and up meet in shared memory, in two turns; the gate's threads finish one half of a turn's tokens, the up's the other.  (A loop: unrolled, with
+                // its registers, this code did not fit the instruction cache and took 27 000 clocks a tile.)
+                constexpr int TURN = H / 2;
+                float *swap = reinterpret_cast<float *>(ring + S::SWAP_AT) + half * TURN * CM;
+                const int up = matrix_of<GATED>(r), g = r & (CM / 2 - 1);
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
+                for (int turn = 0; turn < 2; ++turn) {
 #pragma unroll
-                    for (int i = 0; i < S::N / 2; ++i) swap[(j * (S::N / 2) + i) * CM] = total[h * (S::N / 2) + i];
+                    for (int i = 0; i < TURN; ++i) swap[i * CM + r] = total[turn * TURN + i];
                     sums_barrier();
-                    const int first_i = j * (S::N / 4), end = (int)(a.p.tokens - t0 - h * (S::N / 2) < first_i + S::N / 4 ? a.p.tokens - t0 - h * (S::N / 2) : first_i + S::N / 4);
                     if (ok && row < a.p.rows)
 #pragma unroll 1
-                        for (int i = first_i; i < end && h * (S::N / 2) + i < a.nh; ++i)
-                            store_as(a.p.out, a.p.out_type, (t0 + h * (S::N / 2) + i) * a.p.ldo + row, activation(a.p.act, swap[i * CM]) * swap[(S::N / 2 + i) * CM]);
+                        for (int i = up * (TURN / 2); i < (up + 1) * (TURN / 2) && turn * TURN + i < left; ++i)
+                            store_as(a.p.out, a.p.out_type, (t0 + turn * TURN + i) * a.p.ldo + row, activation(a.p.act, swap[i * CM + g]) * swap[i * CM + CM / 2 + g]);
                     sums_barrier();
                 }
             } else if (ok && row < a.p.rows) {
-                const int64_t t0 = (int64_t)(t % a.nt) * (2 * a.nh) + j * a.nh;
-                const int n = (int)(a.p.tokens - t0 < a.nh ? a.p.tokens - t0 : a.nh);
-                if (a.p.out_type == SKIM_TYPE_F32) store_totals<S::N>(static_cast<float *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, n, total);
-                else if (a.p.out_type == SKIM_TYPE_F16) store_totals<S::N>(static_cast<__half *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, n, total);
-                else store_totals<S::N>(static_cast<__nv_bfloat16 *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, n, total);
+                if (a.p.out_type == SKIM_TYPE_F32) store_totals<H>(static_cast<float *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, left, total);
+                else if (a.p.out_type == SKIM_TYPE_F16) store_totals<H>(static_cast<__half *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, left, total);
+                else store_totals<H>(static_cast<__nv_bfloat16 *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, left, total);
             }
         }
     } else {
-        fewer_registers<24>();
+        fewer_registers<40>();
         if (warp == WARP_TMA && lane == 0) {
             // ------------------------------------------------------------ tokens
-            const uint32_t bytes = (uint32_t)(GATED ? 1 : 2) * 2 * (a.nh / 2) * 128;
+            const uint32_t bytes = 2 * (a.n / 2) * 128;
             int place = 0, issued = 0;
             uint32_t phase = 0;
             for (int t = first; t < tiles && ok; t += clusters) {
-                const int t0 = (t % a.nt) * (GATED ? a.nh : 2 * a.nh) + (int)mine * (a.nh / 2);
+                const int t0 = (t % a.nt) * a.n + (int)mine * (a.n / 2);
                 for (int c = k0; c < k1; ++c) {
                     if (!(ok = wait_for(&sy.b_empty[place], phase ^ 1u, sy))) break;
                     unsigned char *to = ring + (size_t)place * S::B_BYTES;
                     if (mine == 0) barrier_expect(&sy.b_full[place], 2 * bytes);
                     const uint32_t bar = address_in(&sy.b_full[place], leader);
-                    for (int j = 0; j < (GATED ? 1 : 2); ++j)
-                        for (int h = 0; h < 2; ++h) tma_tokens(to + (j * 2 + h) * S::BOX, &tokens_map, bar, c * BK + h * 64, t0 + j * a.nh);
+                    for (int h = 0; h < 2; ++h) tma_tokens(to + h * S::BOX, &tokens_map, bar, c * BK + h * 64, t0);
                     ++issued;
                     if (++place == S::B_PLACES) { place = 0; phase ^= 1u; }
                 }
@@ -347,14 +342,15 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
             if (!ok && mine == 0)                              // copies on their way land before the block ends
                 for (int i = issued > S::B_PLACES ? issued - S::B_PLACES : 0; i < issued; ++i) barrier_wait(&sy.b_full[i % S::B_PLACES], (uint32_t)(i / S::B_PLACES) & 1u, WAIT_CYCLES / 16);
         } else if (warp == WARP_CODES) {
-            // ------------------------------------------------------------ records: a lane has one of each matrix' eight
+            // ------------------------------------------------------------ records: a lane has one of eight
             int place = 0, issued = 0;
             uint32_t phase = 0;
+            const int r = (lane & (RECS - 1)) * SKIM_RECORD_ROWS;
             for (int t = first; t < tiles && ok; t += clusters) {
-                const int64_t rec = ((int64_t)(t / a.nt) * BM + mine * CM) / SKIM_RECORD_ROWS + (lane & (RECS - 1));
-                const bool live = lane < S::MATS * RECS && rec < a.rt;
+                const int64_t rec = row_of<GATED>(t / a.nt, mine, r) / SKIM_RECORD_ROWS;
+                const bool live = lane < RECS && rec < a.rt;
                 const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, live)) * S::RECORD;
-                const unsigned char *src = a.p.tiles[lane < RECS ? 0 : S::MATS - 1] + (rec * a.ct + k0) * S::RECORD;
+                const unsigned char *src = a.p.tiles[matrix_of<GATED>(r)] + (rec * a.ct + k0) * S::RECORD;
                 for (int c = k0; c < k1; ++c, src += S::RECORD) {
                     if (!(ok = warp_wait(&sy.c_empty[place], phase ^ 1u, sy))) break;
                     if (lane == 0) barrier_expect(&sy.c_full[place], bytes);
@@ -368,53 +364,39 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                 for (int i = issued > S::C_PLACES ? issued - S::C_PLACES : 0; i < issued; ++i) barrier_wait(&sy.c_full[i % S::C_PLACES], (uint32_t)(i / S::C_PLACES) & 1u, WAIT_CYCLES / 16);
         } else if (warp == WARP_MMA && mine == 0) {
             // ------------------------------------------------------------ products, for both CTAs.  The whole warp goes through the loops, so that operands are
-            // warp-uniform values, and one lane issues (one lane's own loops: 61 clocks an instruction and 750 a group)
-            const uint32_t instruction = instruction_of(BF16, a.nh);
+            // warp-uniform values, and one lane issues
+            const uint32_t instruction = instruction_of(BF16, a.n);
             const uint16_t both = (uint16_t)(3u << leader);
-            const bool issues = elect_lane();
             int pa = 0, pb = 0, pd = 0;
             uint32_t phase_a = 0, phase_b = 0, phase_d = 1;
-            // one group of one accumulator: tile of A at a_at, tokens j, group k
-            auto group = [&](uint32_t a_at, uint64_t b, int k) {
-                if (!ok || !(ok = warp_wait(&sy.d_empty[pd], phase_d, sy))) return;
-                fence_after();
-                const uint32_t d = tmem + pd * S::N;
-                if (issues) {
-#pragma unroll
-                    for (int u = 0; u < STEPS; ++u) {
-                        const int step = k * STEPS + u;
-                        multiply(d, a_at + step * 8, b + (((step >> 2) * S::BOX + (step & 3) * 32) >> 4), instruction, u > 0);
-                    }
-                    commit_to(&sy.d_full[pd], both);
-                }
-                __syncwarp();
-                if (++pd == S::D_PLACES) { pd = 0; phase_d ^= 1u; }
-            };
             for (int t = first; t < tiles && ok; t += clusters)
                 for (int c = k0; c < k1 && ok; ++c) {
-                    if (!(ok = warp_wait(&sy.b_full[pb], phase_b, sy))) break;
+                    if (!(ok = warp_wait(&sy.b_full[pb], phase_b, sy) && warp_wait(&sy.a_full[pa], phase_a, sy))) break;
                     const uint64_t b = operand_b(smem_address(ring + (size_t)pb * S::B_BYTES));
+                    const uint32_t a_at = tmem + S::A_COL + pa * S::A_COLS;
 #pragma unroll
-                    for (int m = 0; m < S::MATS; ++m) {
-                        if (!ok || !(ok = warp_wait(&sy.a_full[pa], phase_a, sy))) break;
+                    for (int k = 0; k < PER; ++k) {
+                        if (!ok || !(ok = warp_wait(&sy.d_empty[pd], phase_d, sy))) break;
                         fence_after();
-                        const uint32_t a_at = tmem + S::A_COL + pa * S::A_COLS;
+                        if (elect_lane()) {
 #pragma unroll
-                        for (int k = 0; k < PER; ++k) {
-                            group(a_at, b, k);
-                            if (!GATED) group(a_at, b + (2 * S::BOX >> 4), k);
+                            for (int u = 0; u < STEPS; ++u) {
+                                const int step = k * STEPS + u;
+                                multiply(tmem + pd * S::N, a_at + step * 8, b + (((step >> 2) * S::BOX + (step & 3) * 32) >> 4), instruction, u > 0);
+                            }
+                            commit_to(&sy.d_full[pd], both);
+                            if (k == PER - 1) commit_to(&sy.b_empty[pb], both);
                         }
-                        if (GATED && issues) commit_to(&sy.a_empty[pa], both);
                         __syncwarp();
-                        if (++pa == S::A_PLACES) { pa = 0; phase_a ^= 1u; }
+                        if (++pd == S::D_PLACES) { pd = 0; phase_d ^= 1u; }
                     }
-                    if (issues) commit_to(&sy.b_empty[pb], both);
-                    __syncwarp();
+                    if (++pa == S::A_PLACES) { pa = 0; phase_a ^= 1u; }
                     if (++pb == S::B_PLACES) { pb = 0; phase_b ^= 1u; }
                 }
         }
     }
-    // what follows is every warp's, and compiled for the registers of the launch
+    // what follows is every warp's, and compiled for the registers of the launch (a warpgroup's warps meet before they change their registers again)
+    __syncthreads();
     if (warp >= EXPAND_WARPS && warp < EXPAND_WARPS + SUM_WARPS) fewer_registers<128>();
     else more_registers<128>();
     __syncthreads();
@@ -425,29 +407,24 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
     fence_before();
     cluster_barrier();
     if (a.split > 1) {
-        // every pair's totals lie in shared memory, in order of rank; a pair finishes the tokens i with i % split == its number
-        const int r = (int)threadIdx.x & (CM - 1), slice = (int)threadIdx.x / CM;
-        const int64_t row = (int64_t)(first / a.nt) * BM + mine * CM + r, t0 = (int64_t)(first % a.nt) * (GATED ? a.nh : 2 * a.nh);
+        // every pair's totals lie in shared memory; they are added in order of rank.  A pair finishes the tokens i with i % split == its number
+        constexpr int ROWS = GATED ? CM / 2 : CM;
+        const int r = (int)threadIdx.x % ROWS, slice = (int)threadIdx.x / ROWS;
+        const int64_t row = row_of<GATED>(first / a.nt, mine, r), t0 = (int64_t)(first % a.nt) * a.n;
         const float *all = reinterpret_cast<const float *>(ring) + r;
         auto sum_of = [&](int i, int j) {
             float s = 0.0f;
-            for (int p = 0; p < a.split; ++p) s += load_from_rank(all + i * (SUM_WARPS * 32) + j * CM, 2 * p + mine);
+            for (int p = 0; p < a.split; ++p) s += load_from_rank(all + i * CM + j * ROWS, 2 * p + mine);
             return s;
         };
         if (row < a.p.rows)
-            for (int i = part + a.split * slice; i < a.nh; i += a.split * (THREADS / CM)) {
-                if (GATED) {
-                    if (t0 + i < a.p.tokens) store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, activation(a.p.act, sum_of(i, 0)) * sum_of(i, 1));
-                } else {
-                    for (int j = 0; j < 2; ++j)
-                        if (t0 + j * a.nh + i < a.p.tokens) store_as(a.p.out, a.p.out_type, (t0 + j * a.nh + i) * a.p.ldo + row, sum_of(i, j));
-                }
-            }
+            for (int i = part + a.split * slice; i < a.n && t0 + i < a.p.tokens; i += a.split * (THREADS / ROWS))
+                store_as(a.p.out, a.p.out_type, (t0 + i) * a.p.ldo + row, GATED ? activation(a.p.act, sum_of(i, 0)) * sum_of(i, 1) : sum_of(i, 0));
         cluster_barrier();                                     // read before the others end
     }
     if (warp == WARP_MMA) {
         fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM_COLS));
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(sy.tmem), "r"(S::TMEM_COLS));
     }
 }
 
@@ -513,17 +490,20 @@ int skim_launch_grouped_gemm(skim_ctx *ctx, const SkimGroupedProduct &p)
     a.p = p;
     a.ct = (int)skim_record_tiles(p.cols, SKIM_RECORD_COLS);
     a.rt = skim_record_tiles(p.rows, SKIM_RECORD_ROWS);
-    a.mt = (int)skim_record_tiles(p.rows, BM);
-    const int most = p.gated ? Shape<1, true>::N : 2 * Shape<1, false>::N;
-    a.nt = (int)skim_record_tiles(p.tokens, most);
-    const int64_t each = skim_record_tiles(p.tokens, a.nt);
-    a.nh = (int)skim_record_tiles(p.gated ? each : (each + 1) / 2, 32) * 32;
+    a.mt = (int)skim_record_tiles(p.rows, p.gated ? CM : BM);
+    // tokens of a tile: the fewest rounds of tiles, each taking its products (4 clocks a token) or the warp that issues them
+    const int pairs = ctx->sm_count / 2, most = p.group == SKIM_RECORD_COLS ? Shape<1, false>::N : Shape<2, false>::N, fewest = (int)skim_record_tiles(p.tokens, most);
+    int64_t least = INT64_MAX;
+    for (int nt = fewest; nt <= fewest + 2; ++nt) {
+        const int n = (int)skim_record_tiles(skim_record_tiles(p.tokens, nt), 32) * 32;
+        const int64_t cost = ((int64_t)a.mt * nt + pairs - 1) / pairs * (n < 160 ? 640 + 100 : 4 * n + 100);
+        if (cost < least) least = cost, a.nt = nt, a.n = n;
+    }
     if ((int64_t)a.mt * a.nt > 0x1fffffff) return SKIM_ERR_SHAPE;
     a.split = 1;
-    const int pairs = ctx->sm_count / 2;
     while (a.split < MAX_SPLIT && (int64_t)a.mt * a.nt * a.split * 2 <= pairs && a.ct >= a.split * 4) a.split *= 2;
     CUtensorMap map;
-    const int rc = encode_tokens(&map, p, a.nh / 2);
+    const int rc = encode_tokens(&map, p, a.n / 2);
     if (rc) return rc;
     if (p.x_type == SKIM_TYPE_BF16) return p.gated ? launch_by_group<true, true>(ctx, map, a) : launch_by_group<true, false>(ctx, map, a);
     return p.gated ? launch_by_group<false, true>(ctx, map, a) : launch_by_group<false, false>(ctx, map, a);

@@ -237,6 +237,7 @@ __global__ void __launch_bounds__(T) skim_grouped_small_kernel(SmallArgs a)
             if (!(ok = barrier_wait(&full[warp][d], parity))) break;
 #pragma unroll
             for (int r = 0; r < NREC; ++r) take_record<XT, PER, NT>(ring + d * R::PLACE + r * R::RECORD, now, sum_x, total[r]);
+            read_before_copy();
             __syncwarp();
             if (lane == d && done + R::DEPTH < mine) ask();
             ++done;

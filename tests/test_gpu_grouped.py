@@ -274,6 +274,26 @@ def test_few_rows_and_long_rows_share_the_columns(ctx):
         np.testing.assert_allclose(up.cpu().numpy()[far], np.where(g > 0, g.astype(np.float64) ** 2, 0.0)[far], rtol=2.0 ** -23, atol=1e-30)
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_many_tiles_a_pair_of_blocks(ctx, dtype, group):
+    """Several tiles one after another on every SM, run by run: all rows and tokens against 64 bits (on the GPU; the oracle's values)."""
+    rows, cols, tokens = 11008, 1024, 600
+    w = [weights(rows, cols, seed) for seed in (1, 2)]
+    qs = [ctx.grouped_quantize(torch.from_numpy(v).cuda(), group) for v in w]
+    values = [torch.from_numpy(grouped.values(*grouped.quantize(v, group), group)).cuda() for v in w]
+    x, _, _ = token_rows(tokens, cols, dtype)
+    xd = x.double()
+    exact = [xd @ v.t() for v in values]
+    size = [xd.abs() @ v.abs().t() for v in values]
+    as_np = lambda v: v.cpu().numpy()
+    bound = product_bound(cols, group, as_np(size[0]), as_np(exact[0]), torch.float32)
+    want, gated = gated_bound(cols, group, "silu", as_np(exact[0]), as_np(size[0]), as_np(exact[1]), as_np(size[1]), torch.float32)
+    for _ in range(6):
+        assert np.all(np.abs(as_np(ctx.grouped_matvec(qs[0], x).double()) - as_np(exact[0])) <= bound)
+        assert np.all(np.abs(as_np(ctx.grouped_gated(qs[0], qs[1], x).double()) - want) <= gated)
+
+
 def test_a_vector_and_one_row_are_the_same_and_runs_repeat(ctx):
     q, _ = held(weights(70, 700), 64)
     x, _, _ = token_rows(1, 700, torch.float16)
