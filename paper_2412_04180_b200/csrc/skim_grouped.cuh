@@ -84,10 +84,11 @@ __device__ __forceinline__ void bytes_to_halves(uint2 v, uint32_t out[4])
 }
 
 enum { ACT_SILU = SKIM_ACT_SILU, ACT_GELU = SKIM_ACT_GELU };
+// 0.5 (1 + tanh(u)) = 1 / (1 + exp(-2u)): either activation is g / (1 + exp(-v)).
 __device__ __forceinline__ float activation(int act, float g)
 {
-    if (act == ACT_SILU) return g / (1.0f + expf(-g));
-    return 0.5f * g * (1.0f + tanhf(0.7978845608028654f * (g + 0.044715f * g * g * g)));
+    const float v = act == ACT_SILU ? g : 1.5957691216057308f * fmaf(0.044715f * g * g, g, g);
+    return __fdividef(g, 1.0f + expf(-v));
 }
 __device__ __forceinline__ void store_as(void *out, int type, int64_t at, float v)
 {

@@ -21,8 +21,9 @@ using namespace skimg;
 constexpr int CM = 128, BM = 2 * CM;             // weight rows of a CTA, of a pair
 constexpr int BK = SKIM_RECORD_COLS;             // columns of a step: one record
 constexpr int RECS = CM / SKIM_RECORD_ROWS;      // records of a CTA's rows in a step
-constexpr int EXPAND_WARPS = 4, SUM_WARPS = 8, THREADS = (EXPAND_WARPS + SUM_WARPS + 4) * 32;
-constexpr int WARP_TMA = EXPAND_WARPS + SUM_WARPS, WARP_MMA = WARP_TMA + 1, WARP_CODES = WARP_TMA + 2;
+constexpr int EXPAND_WARPS = 4;                  // for a step; two such groups take the steps in turn
+constexpr int FIRST_SUM = 2 * EXPAND_WARPS, SUM_WARPS = 8, THREADS = (FIRST_SUM + SUM_WARPS + 4) * 32;
+constexpr int WARP_TMA = FIRST_SUM + SUM_WARPS, WARP_MMA = WARP_TMA + 1, WARP_CODES = WARP_TMA + 2;
 constexpr int MAX_SPLIT = 4;
 
 // What tensor memory and shared memory hold.  A group's sum goes a round of product, signal, readback and signal; issuing a group's products and signals
@@ -35,7 +36,7 @@ struct Shape {
     static_assert(A_COL + A_PLACES * A_COLS <= TMEM_COLS, "tensor memory");
     static constexpr int BOX = N / 2 * 128;                              // this CTA's tokens, 64 columns
     static constexpr int B_PLACES = PER == 1 && GATED ? 4 : 5, B_BYTES = 2 * BOX;
-    static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, C_PLACES = 5, C_BYTES = RECS * RECORD;
+    static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, C_PLACES = 6, C_BYTES = RECS * RECORD;
     static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? CM * N / 2 * 4 : 0), SYNC_BYTES = 512;
     static constexpr size_t SMEM = 1024 + SYNC_AT + SYNC_BYTES;
     static_assert(SMEM <= 227 * 1024 && N * CM * 4 <= SYNC_AT, "shared memory; the totals of a split tile fit");
@@ -53,7 +54,7 @@ struct GemmArgs {
 struct Sync {
     uint64_t b_full[5], b_empty[5];      // a step's tokens; b_empty: its products are done, which frees its operand A too
     uint64_t a_full[2];
-    uint64_t c_full[5], c_empty[5];      // records
+    uint64_t c_full[6], c_empty[6];      // records
     uint64_t d_full[3], d_empty[3];      // accumulators
     uint32_t tmem;
     int abort;               // a wait ran out
@@ -68,9 +69,10 @@ __device__ __forceinline__ uint32_t address_in(const void *p, uint32_t rank)
 }
 // What is handed over lies in tensor memory and is ordered by tcgen05's fences: no release beyond the block, whose fence would cost hundreds of clocks a time.
 __device__ __forceinline__ void arrive_at(uint32_t addr) { asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory"); }
-__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Sync &sy)
+// (Inline like all that these roles run: a function of its own might use registers that a warp has given up.)
+// The end of a phase, or (false) the limit of the wait, or another role's.
+__device__ __forceinline__ bool wait_longer(uint64_t *bar, uint32_t parity, Sync &sy)
 {
-    if (barrier_try(bar, parity)) return true;
     const long long t0 = clock64();
     while (!barrier_try(bar, parity)) {
         if (*(volatile int *)&sy.abort) return false;
@@ -81,8 +83,15 @@ __device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Sync &s
     }
     return true;
 }
-// By a whole warp, whose lanes go on together.
-__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, Sync &sy) { return __all_sync(0xffffffffu, wait_for(bar, parity, sy)) != 0; }
+__device__ __forceinline__ bool wait_for(uint64_t *bar, uint32_t parity, Sync &sy) { return barrier_try(bar, parity) || wait_longer(bar, parity, sy); }
+// By a whole warp, whose lanes go on together.  The roles whose loops count every clock go on after a wait that ran out, through what is left of their loops, in which no
+// wait lasts any more; those that ask for copies stop.
+__device__ __forceinline__ void warp_wait(uint64_t *bar, uint32_t parity, Sync &sy)
+{
+    wait_for(bar, parity, sy);
+    __syncwarp();
+}
+__device__ __forceinline__ bool warp_wait_or_stop(uint64_t *bar, uint32_t parity, Sync &sy) { return __all_sync(0xffffffffu, wait_for(bar, parity, sy)) != 0; }
 // 64 columns of some token rows into this CTA's shared memory; the bytes are counted at `bar`, in the pair's first CTA.
 __device__ __forceinline__ void tma_tokens(void *dst, const CUtensorMap *map, uint32_t bar, int col, int token)
 {
@@ -138,7 +147,7 @@ template <int N>
 __device__ __forceinline__ void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
 template <int N>
 __device__ __forceinline__ void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
-// A block is launched with 128 registers a thread; of the four warpgroups one takes 104, two 176, one 40.
+// A block is launched with 96 registers a thread; of the five warpgroups two take 72, two 152, one 32.
 __device__ __forceinline__ void sums_barrier() { asm volatile("bar.sync 1, %0;" ::"n"(SUM_WARPS * 32) : "memory"); }
 __device__ __forceinline__ void store_one(float *p, float v) { *p = v; }
 __device__ __forceinline__ void store_one(__half *p, float v) { *p = __float2half_rn(v); }
@@ -191,61 +200,64 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
     skim_wait_for_previous_kernel();
     skim_let_next_kernel_start();
     const uint32_t tmem = 0u;                                // all columns are this block's, so they begin at 0: a constant keeps the operands warp-uniform
-    bool ok = sy.tmem == 0u;
-    if (!ok) *(volatile int *)&sy.abort = 1;
+    if (sy.tmem != 0u) *(volatile int *)&sy.abort = 1;
 
-    if (warp < EXPAND_WARPS) {
-        // ---------------------------------------------------------------- codes to operand A; a thread has a row
-        fewer_registers<104>();
-        int from = 0, step = 0;
-        uint32_t phase_c = 0;
-        const int in = warp * 32 + lane;
-        const uint32_t to = tmem + ((uint32_t)(warp * 32) << 16) + S::A_COL;
-        for (int t = first; t < tiles && ok; t += clusters)
-            for (int c = k0; c < k1; ++c, ++step) {
-                if (!(ok = warp_wait(&sy.c_full[from], phase_c, sy))) break;
-                const unsigned char *r = code_ring + from * S::C_BYTES + in / SKIM_RECORD_ROWS * S::RECORD;
-                uint4 codes[4];
-                uint32_t meta[PER];
+    if (warp < FIRST_SUM) {
+        // ---------------------------------------------------------------- codes to operand A; a thread has a row, its warps every other step and place
+        fewer_registers<72>();
+        static_assert(S::A_PLACES == 2 && S::C_PLACES % 2 == 0, "a place is always the same warps'");
+        const int turn = warp / EXPAND_WARPS, in = (warp & 3) * 32 + lane;
+        const uint32_t to = tmem + ((uint32_t)((warp & 3) * 32) << 16) + S::A_COL + turn * S::A_COLS;
+        const uint32_t full_at = address_in(&sy.a_full[turn], leader);
+        const int steps = (first < tiles ? (tiles - first + clusters - 1) / clusters : 0) * (k1 - k0);
+        int from = turn, freed = turn;                       // places of the records' ring and, of the step two before, the tokens'
+        uint32_t phase_c = 0, phase_b = 0;
+        for (int step = turn; step < steps; step += 2) {
+            warp_wait(&sy.c_full[from], phase_c, sy);
+            const unsigned char *r = code_ring + from * S::C_BYTES + in / SKIM_RECORD_ROWS * S::RECORD;
+            uint4 codes[4];
+            uint32_t meta[PER];
 #pragma unroll
-                for (int p = 0; p < 4; ++p) codes[p] = *reinterpret_cast<const uint4 *>(r + (in % SKIM_RECORD_ROWS) * 64 + p * 16);
+            for (int p = 0; p < 4; ++p) codes[p] = *reinterpret_cast<const uint4 *>(r + (in % SKIM_RECORD_ROWS) * 64 + p * 16);
 #pragma unroll
-                for (int k = 0; k < PER; ++k) meta[k] = reinterpret_cast<const uint32_t *>(r + SKIM_RECORD_CODES)[in % SKIM_RECORD_ROWS * PER + k];
-                const int place = step % S::A_PLACES, before = step - S::A_PLACES;          // the place is free when the step that had it is done
-                if (before >= 0 && !(ok = warp_wait(&sy.b_empty[before % S::B_PLACES], (uint32_t)(before / S::B_PLACES) & 1u, sy))) break;
-                fence_after();
+            for (int k = 0; k < PER; ++k) meta[k] = reinterpret_cast<const uint32_t *>(r + SKIM_RECORD_CODES)[in % SKIM_RECORD_ROWS * PER + k];
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t out[32];
+            for (int h = 0; h < 2; ++h) {
+                uint32_t out[32];
 #pragma unroll
-                    for (int t2 = 0; t2 < 2; ++t2) {
-                        const int tt = 2 * h + t2;
-                        const Zero<BF16> z(meta[tt * PER / 4]);
+                for (int t2 = 0; t2 < 2; ++t2) {
+                    const int tt = 2 * h + t2;
+                    const Zero<BF16> z(meta[tt * PER / 4]);
 #pragma unroll
-                        for (int p = 0; p < 4; ++p) expand(tt == 0 ? codes[p].x : tt == 1 ? codes[p].y : tt == 2 ? codes[p].z : codes[p].w, z, out + 16 * t2 + 4 * p);
-                    }
-                    tmem_store32(to + place * S::A_COLS + 32 * h, out);
+                    for (int p = 0; p < 4; ++p) expand(tt == 0 ? codes[p].x : tt == 1 ? codes[p].y : tt == 2 ? codes[p].z : codes[p].w, z, out + 16 * t2 + 4 * p);
                 }
-                wait_stores();
-                fence_before();
-                read_before_copy();                          // (given back before the values' last use, a place was overwritten before it was read)
-                __syncwarp();
-                if (lane == 0) {
-                    arrive_at(address_in(&sy.a_full[place], leader));
-                    barrier_arrive(&sy.c_empty[from]);
+                if (h == 0 && step >= 2) {                   // the place is free when the step that had it is done
+                    warp_wait(&sy.b_empty[freed], phase_b, sy);
+                    if ((freed += 2) >= S::B_PLACES) { freed -= S::B_PLACES; phase_b ^= 1u; }
+                    fence_after();
                 }
-                if (++from == S::C_PLACES) { from = 0; phase_c ^= 1u; }
+                tmem_store32(to + 32 * h, out);
             }
-    } else if (warp < EXPAND_WARPS + SUM_WARPS) {
+            wait_stores();
+            fence_before();
+            read_before_copy();                              // (given back before the values' last use, a place was overwritten before it was read)
+            __syncwarp();
+            if (lane == 0) {
+                arrive_at(full_at);
+                barrier_arrive(&sy.c_empty[from]);
+            }
+            if ((from += 2) >= S::C_PLACES) { from -= S::C_PLACES; phase_c ^= 1u; }
+        }
+    } else if (warp < FIRST_SUM + SUM_WARPS) {
         // ---------------------------------------------------------------- groups' sums times their scales; a thread has a row and half of the tokens
-        more_registers<176>();
+        more_registers<152>();
         constexpr int H = S::N / 2;
-        const int quarter = warp & 3, half = (warp - EXPAND_WARPS) >> 2, r = quarter * 32 + lane, h = a.n / 2;
+        const int quarter = warp & 3, half = (warp - FIRST_SUM) >> 2, r = quarter * 32 + lane, h = a.n / 2;
         int place = 0;
         uint32_t phase = 0;
         const uint32_t from = tmem + ((uint32_t)(quarter * 32) << 16) + half * h;
         const unsigned char *matrix = a.p.tiles[matrix_of<GATED>(r)];
-        // (every warp goes through all tiles even where a wait ran out: they meet at barriers)
+        const uint32_t empty_at = address_in(&sy.d_empty[0], leader);
         for (int t = first; t < tiles; t += clusters) {
             const int64_t row = row_of<GATED>(t / a.nt, mine, r), rec = row / SKIM_RECORD_ROWS;
             const bool live = rec < a.rt;
@@ -256,7 +268,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
             for (int i = 0; i < H; ++i) total[i] = 0.0f;
 #pragma unroll
             for (int k = 0; k < PER; ++k) meta[k] = __ldg(reinterpret_cast<const uint32_t *>(at) + k);
-            for (int c = k0; c < k1 && ok; ++c) {
+            for (int c = k0; c < k1; ++c) {
                 float scale[PER];
 #pragma unroll
                 for (int k = 0; k < PER; ++k) scale[k] = meta_scale(meta[k]);
@@ -267,24 +279,22 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                 }
 #pragma unroll
                 for (int k = 0; k < PER; ++k) {
-                    if (!ok || !(ok = warp_wait(&sy.d_full[place], phase, sy))) break;
+                    warp_wait(&sy.d_full[place], phase, sy);
                     fence_after();
                     const float s = scale[k];
-                    uint32_t v[2][32];
-                    tmem_load32(from + place * S::N, v[0]);
 #pragma unroll
                     for (int i = 0; i < H; i += 32) {
                         if (i >= h) break;                   // (h is a multiple of 16: the last read may take 16 columns of the other half along, unused)
-                        wait_loads(v[(i / 32) & 1]);
-                        if (i + 32 < H && i + 32 < h) {
-                            tmem_load32(from + place * S::N + i + 32, v[(i / 32 + 1) & 1]);
-                        } else {
+                        uint32_t v[32];
+                        tmem_load32(from + place * S::N + i, v);
+                        wait_loads(v);
+                        if (i + 32 >= H || i + 32 >= h) {
                             fence_before();
                             __syncwarp();
-                            if (lane == 0) arrive_at(address_in(&sy.d_empty[place], leader));
+                            if (lane == 0) arrive_at(empty_at + place * 8);
                         }
 #pragma unroll
-                        for (int u = 0; u < 32; ++u) total[i + u] = fmaf(s, __uint_as_float(v[(i / 32) & 1][u]), total[i + u]);
+                        for (int u = 0; u < 32; ++u) total[i + u] = fmaf(s, __uint_as_float(v[u]), total[i + u]);
                     }
                     if (++place == S::D_PLACES) { place = 0; phase ^= 1u; }
                 }
@@ -308,20 +318,21 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
 #pragma unroll
                     for (int i = 0; i < TURN; ++i) swap[i * CM + r] = total[turn * TURN + i];
                     sums_barrier();
-                    if (ok && row < a.p.rows)
-#pragma unroll 1
+                    if (row < a.p.rows)
+#pragma unroll 4
                         for (int i = up * (TURN / 2); i < (up + 1) * (TURN / 2) && turn * TURN + i < left; ++i)
                             store_as(a.p.out, a.p.out_type, (t0 + turn * TURN + i) * a.p.ldo + row, activation(a.p.act, swap[i * CM + g]) * swap[i * CM + CM / 2 + g]);
                     sums_barrier();
                 }
-            } else if (ok && row < a.p.rows) {
+            } else if (row < a.p.rows) {
                 if (a.p.out_type == SKIM_TYPE_F32) store_totals<H>(static_cast<float *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, left, total);
                 else if (a.p.out_type == SKIM_TYPE_F16) store_totals<H>(static_cast<__half *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, left, total);
                 else store_totals<H>(static_cast<__nv_bfloat16 *>(a.p.out) + t0 * a.p.ldo + row, a.p.ldo, left, total);
             }
         }
     } else {
-        fewer_registers<40>();
+        fewer_registers<32>();
+        bool ok = true;
         if (warp == WARP_TMA && lane == 0) {
             // ------------------------------------------------------------ tokens
             const uint32_t bytes = 2 * (a.n / 2) * 128;
@@ -352,7 +363,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                 const uint32_t bytes = __popc(__ballot_sync(0xffffffffu, live)) * S::RECORD;
                 const unsigned char *src = a.p.tiles[matrix_of<GATED>(r)] + (rec * a.ct + k0) * S::RECORD;
                 for (int c = k0; c < k1; ++c, src += S::RECORD) {
-                    if (!(ok = warp_wait(&sy.c_empty[place], phase ^ 1u, sy))) break;
+                    if (!(ok = warp_wait_or_stop(&sy.c_empty[place], phase ^ 1u, sy))) break;
                     if (lane == 0) barrier_expect(&sy.c_full[place], bytes);
                     __syncwarp();
                     if (live) bulk_copy(code_ring + place * S::C_BYTES + lane * S::RECORD, src, S::RECORD, &sy.c_full[place]);
@@ -369,14 +380,15 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
             const uint16_t both = (uint16_t)(3u << leader);
             int pa = 0, pb = 0, pd = 0;
             uint32_t phase_a = 0, phase_b = 0, phase_d = 1;
-            for (int t = first; t < tiles && ok; t += clusters)
-                for (int c = k0; c < k1 && ok; ++c) {
-                    if (!(ok = warp_wait(&sy.b_full[pb], phase_b, sy) && warp_wait(&sy.a_full[pa], phase_a, sy))) break;
+            for (int t = first; t < tiles; t += clusters)
+                for (int c = k0; c < k1; ++c) {
+                    warp_wait(&sy.b_full[pb], phase_b, sy);
+                    warp_wait(&sy.a_full[pa], phase_a, sy);
                     const uint64_t b = operand_b(smem_address(ring + (size_t)pb * S::B_BYTES));
                     const uint32_t a_at = tmem + S::A_COL + pa * S::A_COLS;
 #pragma unroll
                     for (int k = 0; k < PER; ++k) {
-                        if (!ok || !(ok = warp_wait(&sy.d_empty[pd], phase_d, sy))) break;
+                        warp_wait(&sy.d_empty[pd], phase_d, sy);
                         fence_after();
                         if (elect_lane()) {
 #pragma unroll
@@ -397,8 +409,8 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
     }
     // what follows is every warp's, and compiled for the registers of the launch (a warpgroup's warps meet before they change their registers again)
     __syncthreads();
-    if (warp >= EXPAND_WARPS && warp < EXPAND_WARPS + SUM_WARPS) fewer_registers<128>();
-    else more_registers<128>();
+    if (warp >= FIRST_SUM && warp < FIRST_SUM + SUM_WARPS) fewer_registers<96>();
+    else more_registers<96>();
     __syncthreads();
     if (sy.abort) {
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);      // copies and products in flight end before the block does
