@@ -710,7 +710,7 @@ int grouped_product(skim_ctx *ctx, const SkimGroupedProduct &p)
     SkimGroupedProduct q = p;
     q.status = (unsigned long long *)ctx->ws;
     if (none) return SKIM_OK;
-    return skim_grouped_gemm_takes(q) ? skim_launch_grouped_gemm(ctx, q) : skim_launch_grouped_small(ctx, q);
+    return skim_grouped_gemm_takes(ctx, q) ? skim_launch_grouped_gemm(ctx, q) : skim_launch_grouped_small(ctx, q);
 }
 
 }  // namespace

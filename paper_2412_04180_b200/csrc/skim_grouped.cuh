@@ -72,16 +72,16 @@ __device__ __forceinline__ void expand(uint32_t w, const Zero<true> &z, uint32_t
     for (int i = 0; i < 4; ++i) out[i] = bf162_bits(__hsub2(bits_bf162(and_or(w >> (4 * i), 0x000f000fu, 0x43004300u)), z.near));
 }
 
-// Eight 8-bit activations as pairs of binary16 numbers: b + 128 ORed into the low bits of 1024, less 1152.
-__device__ __forceinline__ void bytes_to_halves(uint2 v, uint32_t out[4])
+// The same as signed bytes, four columns a word.
+__device__ __forceinline__ void expand_bytes(uint32_t w, uint32_t meta, uint32_t out[2])
 {
-    const __half2 off = bits_half2(0x64806480u);
-    const uint32_t a = v.x ^ 0x80808080u, b = v.y ^ 0x80808080u;
-    out[0] = half2_bits(__hsub2(bits_half2(__byte_perm(a, 0x64646464u, 0x4140)), off));
-    out[1] = half2_bits(__hsub2(bits_half2(__byte_perm(a, 0x64646464u, 0x4342)), off));
-    out[2] = half2_bits(__hsub2(bits_half2(__byte_perm(b, 0x64646464u, 0x4140)), off));
-    out[3] = half2_bits(__hsub2(bits_half2(__byte_perm(b, 0x64646464u, 0x4342)), off));
+    const uint32_t z = __byte_perm(meta, 0u, 0x2222);
+    const uint32_t a = (and_or(w, 0x0f0f0f0fu, 0x80808080u) - z) ^ 0x80808080u, b = (and_or(w >> 4, 0x0f0f0f0fu, 0x80808080u) - z) ^ 0x80808080u;      // columns 0 4 1 5, 2 6 3 7
+    out[0] = __byte_perm(a, b, 0x6420);
+    out[1] = __byte_perm(a, b, 0x7531);
 }
+// A whole number below 2^22 in magnitude, by way of 1.5 * 2^23: exact, and without the conversion unit.
+__device__ __forceinline__ float whole_to_float(int v) { return __int_as_float(v + 0x4b400000) - 12582912.0f; }
 
 enum { ACT_SILU = SKIM_ACT_SILU, ACT_GELU = SKIM_ACT_GELU };
 // 0.5 (1 + tanh(u)) = 1 / (1 + exp(-2u)): either activation is g / (1 + exp(-v)).
@@ -171,7 +171,7 @@ struct SkimGroupedProduct {
     int64_t ldo;
     unsigned long long *status;
 };
-bool skim_grouped_gemm_takes(const SkimGroupedProduct &p);
+bool skim_grouped_gemm_takes(const skim_ctx *ctx, const SkimGroupedProduct &p);
 int skim_launch_grouped_gemm(skim_ctx *ctx, const SkimGroupedProduct &p);
 int skim_launch_grouped_small(skim_ctx *ctx, const SkimGroupedProduct &p);
 int skim_launch_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *importance, const float *rscale, int64_t rows, int64_t cols, int64_t ld, int group,

@@ -29,13 +29,15 @@ constexpr int MAX_SPLIT = 4;
 // What tensor memory and shared memory hold.  A group's sum goes a round of product, signal, readback and signal; issuing a group's products and signals
 // takes one warp some 700 clocks however long they are.  So with groups of 128 the accumulators are wide (192 tokens: 768 clocks of products) and two; with
 // smaller groups, where the round counts, narrower and three.
-template <int PER, bool GATED>
+template <int XT, int PER, bool GATED>
 struct Shape {
+    static constexpr bool I8 = XT == SKIM_TYPE_I8;
+    static constexpr int K = I8 ? 32 : 16;                               // columns of an instruction
     static constexpr int N = PER == 1 ? 192 : 128, D_PLACES = PER == 1 ? 2 : 3;      // tokens of an accumulator, at most; accumulators
-    static constexpr int A_PLACES = 2, A_COLS = BK / 2, A_COL = D_PLACES * N, TMEM_COLS = 512;
+    static constexpr int A_PLACES = 2, A_COLS = I8 ? BK / 4 : BK / 2, A_COL = D_PLACES * N, TMEM_COLS = 512;
     static_assert(A_COL + A_PLACES * A_COLS <= TMEM_COLS, "tensor memory");
-    static constexpr int BOX = N / 2 * 128;                              // this CTA's tokens, 64 columns
-    static constexpr int B_PLACES = PER == 1 && GATED ? 4 : 5, B_BYTES = 2 * BOX;
+    static constexpr int BOX = N / 2 * 128, BOXES = I8 ? 1 : 2;          // this CTA's tokens, 128 bytes (64 or 128 columns) of each; boxes of a step
+    static constexpr int B_PLACES = PER == 1 && GATED ? 4 : 5, B_BYTES = BOXES * BOX;
     static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, C_PLACES = 6, C_BYTES = RECS * RECORD;
     static constexpr int CODES_AT = B_PLACES * B_BYTES, SWAP_AT = CODES_AT + C_PLACES * C_BYTES, SYNC_AT = SWAP_AT + (GATED ? CM * N / 2 * 4 : 0), SYNC_BYTES = 512;
     static constexpr size_t SMEM = 1024 + SYNC_AT + SYNC_BYTES;
@@ -104,13 +106,19 @@ __device__ __forceinline__ uint64_t operand_b(uint32_t addr)
 {
     return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)1 << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
 }
-// kind::f16, binary32 accumulators, A and B both binary16 or both bfloat16, K-major, 256 rows, n columns.
-__device__ __forceinline__ uint32_t instruction_of(bool bf16, int n) { return (1u << 4) | (bf16 ? (1u << 7) | (1u << 10) : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(BM >> 4) << 24; }
+// A and B K-major, 256 rows, n columns.  kind::f16: binary32 accumulators, A and B both binary16 or both bfloat16; kind::i8: whole 32-bit accumulators, A and B signed bytes.
+__device__ __forceinline__ uint32_t instruction_of(int xt, int n) { return (xt == SKIM_TYPE_I8 ? 2u << 4 : 1u << 4) | (xt == SKIM_TYPE_F16 ? 0u : (1u << 7) | (1u << 10)) | (uint32_t)(n >> 3) << 17 | (uint32_t)(BM >> 4) << 24; }
+template <bool I8>
 __device__ __forceinline__ void multiply(uint32_t d, uint32_t a, uint64_t b, uint32_t instruction, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(instruction),
-                 "r"(accumulate)
-                 : "memory");
+    if constexpr (I8)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::i8 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(instruction),
+                     "r"(accumulate)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(instruction),
+                     "r"(accumulate)
+                     : "memory");
 }
 // Arrives at this offset in both CTAs of the pair once the products issued so far are done.
 __device__ __forceinline__ void commit_to(uint64_t *bar, uint16_t both)
@@ -169,11 +177,11 @@ __device__ __forceinline__ int64_t row_of(int m, uint32_t mine, int r) { return 
 template <bool GATED>
 __device__ __forceinline__ int matrix_of(int r) { return GATED && r >= CM / 2 ? 1 : 0; }
 
-template <bool BF16, int PER, bool GATED>
+template <int XT, int PER, bool GATED>
 __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __grid_constant__ CUtensorMap tokens_map, GemmArgs a)
 {
-    using S = Shape<PER, GATED>;
-    constexpr int STEPS = BK / 16 / PER;                     // instructions of a group
+    using S = Shape<XT, PER, GATED>;
+    constexpr int STEPS = BK / S::K / PER;                     // instructions of a group
     extern __shared__ unsigned char raw[];
     unsigned char *ring = reinterpret_cast<unsigned char *>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023), *code_ring = ring + S::CODES_AT;
     Sync &sy = *reinterpret_cast<Sync *>(ring + S::SYNC_AT);
@@ -222,14 +230,18 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
 #pragma unroll
             for (int k = 0; k < PER; ++k) meta[k] = reinterpret_cast<const uint32_t *>(r + SKIM_RECORD_CODES)[in % SKIM_RECORD_ROWS * PER + k];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < S::A_COLS / 32; ++h) {
+                constexpr int RUNS = S::I8 ? 4 : 2;          // of 32 columns, in 32 words
                 uint32_t out[32];
 #pragma unroll
-                for (int t2 = 0; t2 < 2; ++t2) {
-                    const int tt = 2 * h + t2;
-                    const Zero<BF16> z(meta[tt * PER / 4]);
+                for (int t2 = 0; t2 < RUNS; ++t2) {
+                    const int tt = RUNS * h + t2;
 #pragma unroll
-                    for (int p = 0; p < 4; ++p) expand(tt == 0 ? codes[p].x : tt == 1 ? codes[p].y : tt == 2 ? codes[p].z : codes[p].w, z, out + 16 * t2 + 4 * p);
+                    for (int p = 0; p < 4; ++p) {
+                        const uint32_t w = tt == 0 ? codes[p].x : tt == 1 ? codes[p].y : tt == 2 ? codes[p].z : codes[p].w;
+                        if constexpr (S::I8) expand_bytes(w, meta[tt * PER / 4], out + 8 * t2 + 2 * p);
+                        else expand(w, Zero<XT == SKIM_TYPE_BF16>(meta[tt * PER / 4]), out + 16 * t2 + 4 * p);
+                    }
                 }
                 if (h == 0 && step >= 2) {                   // the place is free when the step that had it is done
                     warp_wait(&sy.b_empty[freed], phase_b, sy);
@@ -294,13 +306,18 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                             if (lane == 0) arrive_at(empty_at + place * 8);
                         }
 #pragma unroll
-                        for (int u = 0; u < 32; ++u) total[i + u] = fmaf(s, __uint_as_float(v[u]), total[i + u]);
+                        for (int u = 0; u < 32; ++u) total[i + u] = fmaf(s, S::I8 ? whole_to_float((int)v[u]) : __uint_as_float(v[u]), total[i + u]);
                     }
                     if (++place == S::D_PLACES) { place = 0; phase ^= 1u; }
                 }
             }
             const int64_t t0 = (int64_t)(t % a.nt) * a.n + half * h;
             const int left = (int)(a.p.tokens - t0 < h ? a.p.tokens - t0 : h);             // this thread's tokens (none: below 1)
+            if (a.p.x_scale) {
+#pragma unroll
+                for (int i = 0; i < H; ++i)
+                    if (i < left) total[i] *= __ldg(a.p.x_scale + t0 + i);
+            }
             if (a.split > 1) {
                 // the pairs of the cluster have one tile; the rings are no longer used: totals go there, [token][row]
                 float *all = reinterpret_cast<float *>(ring) + half * h * CM + r;
@@ -335,7 +352,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
         bool ok = true;
         if (warp == WARP_TMA && lane == 0) {
             // ------------------------------------------------------------ tokens
-            const uint32_t bytes = 2 * (a.n / 2) * 128;
+            const uint32_t bytes = S::BOXES * (a.n / 2) * 128;
             int place = 0, issued = 0;
             uint32_t phase = 0;
             for (int t = first; t < tiles && ok; t += clusters) {
@@ -345,7 +362,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
                     unsigned char *to = ring + (size_t)place * S::B_BYTES;
                     if (mine == 0) barrier_expect(&sy.b_full[place], 2 * bytes);
                     const uint32_t bar = address_in(&sy.b_full[place], leader);
-                    for (int h = 0; h < 2; ++h) tma_tokens(to + h * S::BOX, &tokens_map, bar, c * BK + h * 64, t0);
+                    for (int h = 0; h < S::BOXES; ++h) tma_tokens(to + h * S::BOX, &tokens_map, bar, c * BK + h * 64, t0);
                     ++issued;
                     if (++place == S::B_PLACES) { place = 0; phase ^= 1u; }
                 }
@@ -376,7 +393,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
         } else if (warp == WARP_MMA && mine == 0) {
             // ------------------------------------------------------------ products, for both CTAs.  The whole warp goes through the loops, so that operands are
             // warp-uniform values, and one lane issues
-            const uint32_t instruction = instruction_of(BF16, a.n);
+            const uint32_t instruction = instruction_of(XT, a.n);
             const uint16_t both = (uint16_t)(3u << leader);
             int pa = 0, pb = 0, pd = 0;
             uint32_t phase_a = 0, phase_b = 0, phase_d = 1;
@@ -394,7 +411,7 @@ __global__ void __launch_bounds__(THREADS, 1) skim_grouped_gemm_kernel(const __g
 #pragma unroll
                             for (int u = 0; u < STEPS; ++u) {
                                 const int step = k * STEPS + u;
-                                multiply(tmem + pd * S::N, a_at + step * 8, b + (((step >> 2) * S::BOX + (step & 3) * 32) >> 4), instruction, u > 0);
+                                multiply<S::I8>(tmem + pd * S::N, a_at + step * 8, b + (((step >> 2) * S::BOX + (step & 3) * 32) >> 4), instruction, u > 0);
                             }
                             commit_to(&sy.d_full[pd], both);
                             if (k == PER - 1) commit_to(&sy.b_empty[pb], both);
@@ -445,19 +462,20 @@ int encode_tokens(CUtensorMap *map, const SkimGroupedProduct &p, int box_rows)
     void *fn = nullptr;
     cudaDriverEntryPointQueryResult qres;
     if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) return SKIM_ERR_CUDA;
-    const cuuint64_t dims[2] = {(cuuint64_t)p.cols, (cuuint64_t)p.tokens}, strides[1] = {(cuuint64_t)p.ldx * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+    const int bytes = p.x_type == SKIM_TYPE_I8 ? 1 : 2;
+    const cuuint64_t dims[2] = {(cuuint64_t)p.cols, (cuuint64_t)p.tokens}, strides[1] = {(cuuint64_t)p.ldx * bytes};
+    const cuuint32_t box[2] = {(cuuint32_t)(128 / bytes), (cuuint32_t)box_rows}, steps[2] = {1, 1};
     const CUresult r = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn)(
-        map, p.x_type == SKIM_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(p.x), dims, strides, box, steps,
-        CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+        map, p.x_type == SKIM_TYPE_I8 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : p.x_type == SKIM_TYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+        const_cast<void *>(p.x), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? SKIM_OK : SKIM_ERR_CUDA;
 }
 
-template <bool BF16, int PER, bool GATED>
+template <int XT, int PER, bool GATED>
 int launch(skim_ctx *ctx, const CUtensorMap &map, const GemmArgs &a)
 {
-    auto kernel = skim_grouped_gemm_kernel<BF16, PER, GATED>;
-    constexpr size_t SMEM = Shape<PER, GATED>::SMEM;
+    auto kernel = skim_grouped_gemm_kernel<XT, PER, GATED>;
+    constexpr size_t SMEM = Shape<XT, PER, GATED>::SMEM;
     SKIM_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SMEM));
     const int pairs = ctx->sm_count / 2, tiles = a.mt * a.nt;
     cudaLaunchConfig_t cfg = {};
@@ -477,46 +495,71 @@ int launch(skim_ctx *ctx, const CUtensorMap &map, const GemmArgs &a)
     ctx->launches += 1;
     return SKIM_OK;
 }
-template <bool BF16, bool GATED>
+template <int XT, bool GATED>
 int launch_by_group(skim_ctx *ctx, const CUtensorMap &map, const GemmArgs &a)
 {
     switch (a.p.group) {
-    case 128: return launch<BF16, 1, GATED>(ctx, map, a);
-    case 64: return launch<BF16, 2, GATED>(ctx, map, a);
-    default: return launch<BF16, 4, GATED>(ctx, map, a);
+    case 128: return launch<XT, 1, GATED>(ctx, map, a);
+    case 64: return launch<XT, 2, GATED>(ctx, map, a);
+    default: return launch<XT, 4, GATED>(ctx, map, a);
     }
+}
+template <int XT>
+int launch_by_matrices(skim_ctx *ctx, const CUtensorMap &map, const GemmArgs &a)
+{
+    return a.p.gated ? launch_by_group<XT, true>(ctx, map, a) : launch_by_group<XT, false>(ctx, map, a);
+}
+
+// Tiles, and the time that they take, in clocks: a round of tiles takes 4 a token and column step of a group of 128 (or the 740 of the warp that issues the products), more in
+// smaller groups, 5000 for its end, and a launch with its start 9000.  Pairs that share columns cost 5000 more, and four of them only as many clusters as the chip's
+// parts hold at once (16 of them, on 4096 x 4096: 25 us, pairs of two 17).
+int64_t plan_of(const skim_ctx *ctx, const SkimGroupedProduct &p, GemmArgs &a)
+{
+    a.p = p;
+    a.ct = (int)skim_record_tiles(p.cols, SKIM_RECORD_COLS);
+    a.rt = skim_record_tiles(p.rows, SKIM_RECORD_ROWS);
+    a.mt = (int)skim_record_tiles(p.rows, p.gated ? CM : BM);
+    const int per = SKIM_RECORD_COLS / p.group, most = per == 1 ? Shape<0, 1, false>::N : Shape<0, 2, false>::N;
+    const int64_t pairs = ctx->sm_count / 2, fewest = skim_record_tiles(p.tokens, most);
+    int64_t least = INT64_MAX;
+    for (int64_t nt = fewest; nt <= fewest + 2; ++nt) {
+        const int n = (int)skim_record_tiles(skim_record_tiles(p.tokens, nt), 32) * 32;
+        const int64_t tiles = a.mt * nt;
+        if (tiles > 0x1fffffff) break;
+        int split = 1;
+        while (split < MAX_SPLIT && tiles * split * 2 <= pairs && a.ct >= split * 4 && (split == 1 || tiles <= 8)) split *= 2;
+        const int step = per == 1 ? (n < 160 ? 740 : 4 * n + 100) : per == 2 ? 1100 : 2000;
+        const int64_t cost = 9000 + (tiles * split + pairs - 1) / pairs * ((int64_t)((a.ct + split - 1) / split) * step + 5000) + (split > 1 ? 5000 : 0);
+        if (cost < least) least = cost, a.nt = (int)nt, a.n = n, a.split = split;
+    }
+    return least;
 }
 
 }  // namespace
 
-bool skim_grouped_gemm_takes(const SkimGroupedProduct &p)
+// Whether the tensor-memory kernel takes the call: tokens enough, rows that TMA can read, and less time than passes of 16 tokens through the other kernel, which take about
+// 4000 clocks and 1.5 a record each (us, this kernel and the other: 11008 x 4096, 64 tokens 22 and 47; 4096 x 4096, 32 tokens 17 and 12; 1024 x 1024, 128 tokens 11 and 6).
+bool skim_grouped_gemm_takes(const skim_ctx *ctx, const SkimGroupedProduct &p)
 {
-    if (p.x_type == SKIM_TYPE_I8 || p.x_scale) return false;
-    if ((reinterpret_cast<uintptr_t>(p.x) & 15u) || p.ldx % 8 || p.tokens > 0x3fffffff || p.rows > 0x3fffffff) return false;
-    return p.tokens > 64;
+    const int bytes = p.x_type == SKIM_TYPE_I8 ? 1 : 2;
+    if (p.tokens <= 16 || (reinterpret_cast<uintptr_t>(p.x) & 15u) || (p.ldx * bytes) % 16 || p.rows > 0x3fffffff) return false;
+    GemmArgs a;
+    const int64_t cost = plan_of(ctx, p, a);
+    if (cost == INT64_MAX) return false;
+    const int64_t passes = (p.tokens + 15) / 16;
+    return cost < 4000 + passes * (a.rt * a.ct) * (p.gated ? 6 : 3) / 2;
 }
 
 int skim_launch_grouped_gemm(skim_ctx *ctx, const SkimGroupedProduct &p)
 {
     GemmArgs a;
-    a.p = p;
-    a.ct = (int)skim_record_tiles(p.cols, SKIM_RECORD_COLS);
-    a.rt = skim_record_tiles(p.rows, SKIM_RECORD_ROWS);
-    a.mt = (int)skim_record_tiles(p.rows, p.gated ? CM : BM);
-    // tokens of a tile: the fewest rounds of tiles, each taking its products (4 clocks a token) or the warp that issues them
-    const int pairs = ctx->sm_count / 2, most = p.group == SKIM_RECORD_COLS ? Shape<1, false>::N : Shape<2, false>::N, fewest = (int)skim_record_tiles(p.tokens, most);
-    int64_t least = INT64_MAX;
-    for (int nt = fewest; nt <= fewest + 2; ++nt) {
-        const int n = (int)skim_record_tiles(skim_record_tiles(p.tokens, nt), 32) * 32;
-        const int64_t cost = ((int64_t)a.mt * nt + pairs - 1) / pairs * (n < 160 ? 640 + 100 : 4 * n + 100);
-        if (cost < least) least = cost, a.nt = nt, a.n = n;
-    }
-    if ((int64_t)a.mt * a.nt > 0x1fffffff) return SKIM_ERR_SHAPE;
-    a.split = 1;
-    while (a.split < MAX_SPLIT && (int64_t)a.mt * a.nt * a.split * 2 <= pairs && a.ct >= a.split * 4) a.split *= 2;
+    if (plan_of(ctx, p, a) == INT64_MAX) return SKIM_ERR_SHAPE;
     CUtensorMap map;
     const int rc = encode_tokens(&map, p, a.n / 2);
     if (rc) return rc;
-    if (p.x_type == SKIM_TYPE_BF16) return p.gated ? launch_by_group<true, true>(ctx, map, a) : launch_by_group<true, false>(ctx, map, a);
-    return p.gated ? launch_by_group<false, true>(ctx, map, a) : launch_by_group<false, false>(ctx, map, a);
+    switch (p.x_type) {
+    case SKIM_TYPE_F16: return launch_by_matrices<SKIM_TYPE_F16>(ctx, map, a);
+    case SKIM_TYPE_BF16: return launch_by_matrices<SKIM_TYPE_BF16>(ctx, map, a);
+    default: return launch_by_matrices<SKIM_TYPE_I8>(ctx, map, a);
+    }
 }

@@ -18,7 +18,6 @@ namespace {
 
 using namespace skimg;
 
-constexpr int T = 128, NW = T / 32;
 constexpr int MAX_SPLIT = 8;
 
 struct SmallArgs {
@@ -30,10 +29,15 @@ struct SmallArgs {
     int whole;               // records whose activations can be loaded as whole pieces
 };
 
-// The ring of a warp: `DEPTH` places for a record of each matrix.
-template <int PER, int NREC>
+// The ring of a warp: `DEPTH` places for a record of each matrix; its activations in registers: SETS, of which one is in use and the others on their way.
+// One matrix: blocks of 8 warps, which share the columns of a row of records (4096 x 4096, one token: 4.7 us, with 4 warps 5.5).  Two matrices: 4 warps, and registers
+// for five blocks of an SM, so that 11008 rows are one round of blocks (11008 x 4096, one token: 13.9 us; with 8 warps 17.9, without the limit 20.6).
+template <int XT, int PER, int NREC, int NT>
 struct Ring {
+    static constexpr int NW = NREC == 1 ? 8 : 4, T = NW * 32, BLOCKS = NREC == 1 ? 2 : NT == 1 || XT == SKIM_TYPE_I8 ? 5 : 3;
+    static constexpr int SETS = NREC == 1 && NT * (XT == SKIM_TYPE_I8 ? 1 : 2) <= 2 ? 3 : 2;
     static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, DEPTH = NREC == 1 ? 6 : 4, PLACE = NREC * RECORD, BYTES = DEPTH * PLACE;
+    static_assert(DEPTH % SETS == 0, "a place goes with a set");
 };
 
 __device__ __forceinline__ void mma(float c[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1, __half)
@@ -118,8 +122,7 @@ __device__ __forceinline__ void take_record(const unsigned char *rec, const Piec
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int u = 0; u < 4; ++u)                  // below 2^18: exact, by way of 1.5 * 2^23
-                    acc[n][u] = __int_as_float(whole[n][u] - (u < 2 ? za : zb) * sum_x[n][k][u & 1] + 0x4b400000) - 12582912.0f;
+                for (int u = 0; u < 4; ++u) acc[n][u] = whole_to_float(whole[n][u] - (u < 2 ? za : zb) * sum_x[n][k][u & 1]);      // below 2^18
         } else {
             using M = typename std::conditional<XT == SKIM_TYPE_BF16, __nv_bfloat16, __half>::type;
             const Zero<XT == SKIM_TYPE_BF16> za(ma), zb(mb);
@@ -147,12 +150,12 @@ __device__ __forceinline__ void take_record(const unsigned char *rec, const Piec
 }
 
 template <int XT, int PER, int NREC, int NT>
-__global__ void __launch_bounds__(T) skim_grouped_small_kernel(SmallArgs a)
+__global__ void __launch_bounds__(Ring<XT, PER, NREC, NT>::T, Ring<XT, PER, NREC, NT>::BLOCKS) skim_grouped_small_kernel(SmallArgs a)
 {
-    using R = Ring<PER, NREC>;
+    using R = Ring<XT, PER, NREC, NT>;
+    constexpr int T = R::T, NW = R::NW;
     constexpr int X_BYTES = XT == SKIM_TYPE_I8 ? 1 : 2;
     static_assert(NREC * NT * 512 <= R::BYTES, "the warp's ring holds its totals at the end");
-    static_assert(R::DEPTH % 2 == 0, "activations alternate between two sets of registers");
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) uint64_t full[NW][R::DEPTH];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
@@ -188,7 +191,7 @@ __global__ void __launch_bounds__(T) skim_grouped_small_kernel(SmallArgs a)
 #pragma unroll
     for (int n = 0; n < NT; ++n)
         xr[n] = static_cast<const unsigned char *>(a.p.x) + ((t0 + (8 * n + g < tokens ? 8 * n + g : tokens - 1)) * a.p.ldx + (int64_t)k0 * SKIM_RECORD_COLS + 8 * q) * X_BYTES;
-    Pieces<XT> x[2][NT];
+    Pieces<XT> x[R::SETS][NT];
     auto ask_x = [&](int i, Pieces<XT> o[NT]) {
         if (i >= mine) return;
         if (k0 + i < a.whole) {
@@ -201,7 +204,8 @@ __global__ void __launch_bounds__(T) skim_grouped_small_kernel(SmallArgs a)
 #pragma unroll
         for (int n = 0; n < NT; ++n) xr[n] += SKIM_RECORD_COLS * X_BYTES;
     };
-    ask_x(0, x[0]);
+#pragma unroll
+    for (int i = 0; i < R::SETS - 1; ++i) ask_x(i, x[i]);
 
     float total[NREC][NT][4] = {};
     bool ok = true;
@@ -211,8 +215,8 @@ __global__ void __launch_bounds__(T) skim_grouped_small_kernel(SmallArgs a)
 #pragma unroll
         for (int d = 0; d < R::DEPTH; ++d) {
             if (done >= mine) break;
-            ask_x(done + 1, x[(d + 1) & 1]);
-            Pieces<XT> (&now)[NT] = x[d & 1];
+            ask_x(done + R::SETS - 1, x[(d + R::SETS - 1) % R::SETS]);
+            Pieces<XT> (&now)[NT] = x[d % R::SETS];
             int sum_x[NT][PER][2];
             if constexpr (XT == SKIM_TYPE_I8) {
 #pragma unroll
@@ -287,22 +291,23 @@ __global__ void __launch_bounds__(T) skim_grouped_small_kernel(SmallArgs a)
 }
 
 // How the warps share rows and columns, by the clocks of an SM: a warp alone takes about 350 a record (its chain of copies, expansion and products); warps
-// together share the issue slots at about 28 a record, and 60 for the start and the end of each.
+// together share the issue slots at about 28 a record, and 60 for the start and the end of each.  A cluster's barriers and sums cost 2500: blocks share columns only
+// where rows are few and long.  (us, kw warps a block and split blocks, measured: 4096 x 4096, one token, 4 warps: kw 4 5.5, kw 2 split 2 6.5, kw 1 split 4 6.8;
+// gated 11008 x 4096: kw 4 13.9, kw 2 15.8, kw 2 split 2 14.8.)
 struct Plan {
     int kw, split;
 };
-constexpr int RECORD_ALONE = 350, RECORD_SHARED = 28, WARP_ENDS = 60;
-Plan plan_of(const skim_ctx *ctx, int64_t rt, int ct, int nrec, int nt)
+constexpr int RECORD_ALONE = 350, RECORD_SHARED = 28, WARP_ENDS = 60, CLUSTER_COST = 2500;
+Plan plan_of(const skim_ctx *ctx, int64_t rt, int ct, int nrec, int nt, int nw, int resident)
 {
     Plan best = {1, 1};
     int64_t least = INT64_MAX;
-    const int resident = nrec == 1 ? 8 : 6;                  // blocks of an SM
-    for (int kw = 1; kw <= NW; kw *= 2)
-        for (int s = 1; s <= MAX_SPLIT; ++s) {
+    for (int kw = 1; kw <= nw; kw *= 2)
+        for (int s = 1; s <= MAX_SPLIT; s *= 2) {
             if (kw * s > ct) break;                          // every part has a record
-            const int64_t chunks = (ct + kw * s - 1) / (kw * s), blocks = (rt * kw + NW - 1) / NW * s, rounds = (blocks + ctx->sm_count - 1) / ctx->sm_count;
-            const int64_t waves = (rounds + resident - 1) / resident, together = (rounds + waves - 1) / waves * NW * RECORD_SHARED;
-            const int64_t cost = waves * chunks * nrec * nt * (together > RECORD_ALONE ? together : RECORD_ALONE) + rounds * NW * WARP_ENDS;
+            const int64_t chunks = (ct + kw * s - 1) / (kw * s), blocks = (rt * kw + nw - 1) / nw * s, rounds = (blocks + ctx->sm_count - 1) / ctx->sm_count;
+            const int64_t waves = (rounds + resident - 1) / resident, together = (rounds + waves - 1) / waves * nw * RECORD_SHARED;
+            const int64_t cost = waves * chunks * nrec * nt * (together > RECORD_ALONE ? together : RECORD_ALONE) + rounds * nw * WARP_ENDS + (s > 1 ? CLUSTER_COST : 0);
             if (cost < least) best = {kw, s}, least = cost;
         }
     return best;
@@ -312,14 +317,16 @@ template <int XT, int PER, int NREC, int NT>
 int launch(skim_ctx *ctx, const SmallArgs &all)
 {
     SmallArgs a = all;
-    const Plan plan = plan_of(ctx, a.rt, a.ct, NREC, NT);
+    using R = Ring<XT, PER, NREC, NT>;
+    constexpr size_t smem = (size_t)R::NW * R::BYTES;
+    constexpr int T = R::T, NW = R::NW;
+    const Plan plan = plan_of(ctx, a.rt, a.ct, NREC, NT, NW, NREC == 1 ? 3 : R::BLOCKS);
     a.split = plan.split;
     a.kw = plan.kw;
     const int64_t blocks = (a.rt * a.kw + NW - 1) / NW;
     if (blocks * a.split > 0x7fffffff) return SKIM_ERR_SHAPE;
-    constexpr size_t smem = (size_t)NW * Ring<PER, NREC>::BYTES;
-    static_assert(smem <= 48 * 1024 - 1024, "no permission needed");
     auto kernel = skim_grouped_small_kernel<XT, PER, NREC, NT>;
+    if (smem > 47 * 1024) SKIM_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     constexpr int64_t most = 65535 * (8 * NT);               // tokens of a launch
     for (int64_t first = 0; first < all.p.tokens; first += most) {
         a.p.x = static_cast<const unsigned char *>(all.p.x) + first * all.p.ldx * (XT == SKIM_TYPE_I8 ? 1 : 2);

@@ -311,29 +311,32 @@ class Skim:
         return out
 
     # ---- weights of 4 bits with group scales, their products with token rows, and the norm in front of them
+    # (The calls that a decoded token makes are bound by the host: their checks ask a tensor for as little as they can.)
     def _new(self, shape, dtype):
         """A tensor of the context's device, made on the context's stream (which writes it)."""
-        if self._stream is None:
+        if self._stream is None or torch.cuda.current_stream(self.device).cuda_stream == self._stream.cuda_stream:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self._stream):
             return torch.empty(shape, dtype=dtype, device=self.device)
 
     def _rows_of(self, t, name, dtypes, cols=None):
         """(rows, stride in elements) of a matrix, or of a vector as one row; elements of a row lie side by side."""
-        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype in dtypes):
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype not in dtypes:
             raise TypeError(f"{name}: expected a tensor on {self.device} of dtype {' or '.join(str(d) for d in dtypes)}")
-        shape = t.shape
-        if not 1 <= len(shape) <= 2 or (cols is not None and shape[-1] != cols):
-            raise TypeError(f"{name}: expected a vector or a matrix" + ("" if cols is None else f" of {cols} columns") + f", got shape {tuple(shape)}")
-        rows = shape[0] if len(shape) == 2 else 1
-        if t.stride(-1) != 1 and shape[-1] > 1:
+        n = t.dim()
+        if not 1 <= n <= 2 or (cols is not None and t.size(-1) != cols):
+            raise TypeError(f"{name}: expected a vector or a matrix" + ("" if cols is None else f" of {cols} columns") + f", got shape {tuple(t.shape)}")
+        if t.stride(-1) != 1 and t.size(-1) > 1:
             raise TypeError(f"{name}: the elements of a row have to lie side by side")
-        if rows <= 1:
-            return rows, shape[-1]
-        return rows, t.stride(0)
+        if n == 2:
+            rows = t.size(0)
+            if rows > 1:
+                return rows, t.stride(0)
+            return rows, t.size(1)
+        return 1, t.size(0)
 
     def _plain(self, t, name, dtype, n):
-        if not (isinstance(t, torch.Tensor) and t.device == self.device and t.dtype == dtype and t.is_contiguous() and t.numel() == n):
+        if not (isinstance(t, torch.Tensor) and t.get_device() == self.device.index and t.dtype is dtype and t.is_contiguous() and t.numel() == n):
             raise TypeError(f"{name}: expected a contiguous tensor on {self.device} of dtype {dtype} with {n} elements")
         return t.data_ptr()
 
@@ -355,7 +358,7 @@ class Skim:
 
     def _tiles(self, q, name):
         t, rows, cols, group = q["tiles"], q["rows"], q["cols"], q["group"]
-        if not (t.device == self.device and t.dtype == torch.uint8 and t.is_contiguous()):
+        if t.get_device() != self.device.index or t.dtype is not torch.uint8 or not t.is_contiguous():
             raise TypeError(f"{name}: expected contiguous uint8 tiles on {self.device}")
         if group not in (32, 64, 128) or t.numel() < -(-rows // 16) * -(-cols // 128) * (1024 + 8192 // group):
             raise TypeError(f"{name}: {t.numel()} bytes of tiles do not hold {rows} x {cols} weights in groups of {group}")
@@ -405,7 +408,7 @@ class Skim:
         tiles, rows, cols, group = self._tiles(q, "q")
         tokens, ldx, kind, scale = self._tokens(x, x_scale, cols)
         out, y, ldy = self._out_rows(out, out_dtype if out is None else out.dtype, x, tokens, rows)
-        _chk(lib().skim_grouped_matvec(self._h, tiles, rows, cols, group, x.data_ptr(), kind, ldx, scale, tokens, y, TYPES.get(out.dtype, -1), ldy),
+        _chk((_lib or lib()).skim_grouped_matvec(self._h, tiles, rows, cols, group, x.data_ptr(), kind, ldx, scale, tokens, y, TYPES.get(out.dtype, -1), ldy),
              "skim_grouped_matvec")
         return out
 
@@ -417,7 +420,7 @@ class Skim:
             raise TypeError(f"up: holds rows, cols, group {held}, gate {[rows, cols, group]}")
         tokens, ldx, kind, scale = self._tokens(x, x_scale, cols)
         out, y, ldy = self._out_rows(out, out_dtype if out is None else out.dtype, x, tokens, rows)
-        _chk(lib().skim_grouped_gated(self._h, tiles, other, rows, cols, group, ACTIVATIONS.get(activation, -1), x.data_ptr(), kind, ldx, scale,
+        _chk((_lib or lib()).skim_grouped_gated(self._h, tiles, other, rows, cols, group, ACTIVATIONS.get(activation, -1), x.data_ptr(), kind, ldx, scale,
                                       tokens, y, TYPES.get(out.dtype, -1), ldy), "skim_grouped_gated")
         return out
 
@@ -442,7 +445,7 @@ class Skim:
                 raise TypeError(f"sum_out: expected {rows} rows, got {got}")
         if out.dtype == torch.int8 and out_scale is None:
             out_scale = self._new((rows,), torch.float32)
-        _chk(lib().skim_add_rmsnorm(self._h, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
+        _chk((_lib or lib()).skim_add_rmsnorm(self._h, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
                                     None if weight is None else self._plain(weight, "weight", kind, cols), TYPES[kind], rows, cols, eps,
                                     None if sum_out is None else sum_out.data_ptr(), lds, y, TYPES.get(out.dtype, -1), ldo,
                                     None if out_scale is None else self._plain(out_scale, "out_scale", torch.float32, rows)), "skim_add_rmsnorm")

@@ -275,23 +275,28 @@ def test_few_rows_and_long_rows_share_the_columns(ctx):
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
-@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
-def test_many_tiles_a_pair_of_blocks(ctx, dtype, group):
-    """Several tiles one after another on every SM, run by run: all rows and tokens against 64 bits (on the GPU; the oracle's values)."""
-    rows, cols, tokens = 11008, 1024, 600
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16, torch.int8])
+@pytest.mark.parametrize("rows,cols,tokens,pad,runs", [(11008, 1024, 600, 0, 5),          # several tiles one after another on every SM
+                                                       (3001, 520, 700, 16, 2),           # ragged in every direction
+                                                       (520, 4101, 300, 11, 2),           # few tiles: four pairs of blocks share the columns
+                                                       (1030, 4096, 601, 0, 2),           # two pairs
+                                                       (12000, 2000, 20, 0, 2)])          # few tokens, many rows
+def test_many_tokens(ctx, rows, cols, tokens, pad, runs, dtype, group):
+    """All rows and tokens, run by run, against 64 bits (products on the GPU, of the oracle's values)."""
     w = [weights(rows, cols, seed) for seed in (1, 2)]
     qs = [ctx.grouped_quantize(torch.from_numpy(v).cuda(), group) for v in w]
     values = [torch.from_numpy(grouped.values(*grouped.quantize(v, group), group)).cuda() for v in w]
-    x, _, _ = token_rows(tokens, cols, dtype)
-    xd = x.double()
+    x, xv, scale = token_rows(tokens, cols, dtype, pad=pad)
+    xs = None if scale is None else torch.from_numpy(scale).cuda()
+    xd = torch.from_numpy(xv).cuda() * (1.0 if xs is None else xs.double()[:, None])
     exact = [xd @ v.t() for v in values]
     size = [xd.abs() @ v.abs().t() for v in values]
     as_np = lambda v: v.cpu().numpy()
     bound = product_bound(cols, group, as_np(size[0]), as_np(exact[0]), torch.float32)
-    want, gated = gated_bound(cols, group, "silu", as_np(exact[0]), as_np(size[0]), as_np(exact[1]), as_np(size[1]), torch.float32)
-    for _ in range(6):
-        assert np.all(np.abs(as_np(ctx.grouped_matvec(qs[0], x).double()) - as_np(exact[0])) <= bound)
-        assert np.all(np.abs(as_np(ctx.grouped_gated(qs[0], qs[1], x).double()) - want) <= gated)
+    want, gated = gated_bound(cols, group, "gelu", as_np(exact[0]), as_np(size[0]), as_np(exact[1]), as_np(size[1]), torch.bfloat16)
+    for _ in range(runs):
+        assert np.all(np.abs(as_np(ctx.grouped_matvec(qs[0], x, x_scale=xs).double()) - as_np(exact[0])) <= bound)
+        assert np.all(np.abs(as_np(ctx.grouped_gated(qs[0], qs[1], x, x_scale=xs, activation="gelu", out_dtype=torch.bfloat16).double()) - want) <= gated)
 
 
 def test_a_vector_and_one_row_are_the_same_and_runs_repeat(ctx):
