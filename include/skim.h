@@ -25,6 +25,7 @@
  *   skim_grouped_quantize, skim_grouped_dequantize, skim_grouped_matvec, skim_grouped_gated   uniform 4-bit weights with a scale per
  *                         group of columns, which the paper compares its codebooks with, and their products with token rows
  *   skim_add_rmsnorm      the norm in front of those products, with 16-bit or 8-bit rows as its result
+ *   skim_feed_forward     the norm, the gated product and the product behind it, as a decoder layer runs them
  *   skim_residual, skim_err_lfull   the error of a row in the L-full form, (w - wq) X X^T (w - wq)^T
  *                                                               (Section 3.4; Section 4.2; Algorithm 3)
  *
@@ -359,6 +360,17 @@ int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t 
  */
 int skim_add_rmsnorm(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int type, int64_t rows,
                      int64_t cols, float eps, void *sum_out, int64_t lds, void *out, int out_type, int64_t ldo, float *out_scale);
+
+/*
+ * The feed-forward half of a decoder layer: skim_add_rmsnorm of x + residual, to 8 bits (eight_bit != 0) or to `type`; skim_grouped_gated of the result with gate and
+ * up [hidden][cols], to `type`; skim_grouped_matvec of that with down [cols][hidden], y [tokens][ldy] in `type`.  Arguments and roundings as there; the three matrices have
+ * one group size.  y must not overlap x, residual or sum_out; sum_out may be x or residual (same pointer and stride).
+ *   scratch  device, 256-byte aligned, at least skim_feed_forward_bytes bytes, which the calls in flight do not share: the rows between the three
+ */
+int skim_feed_forward_bytes(int64_t tokens, int64_t cols, int64_t hidden, size_t *out);
+int skim_feed_forward(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int type, int64_t tokens, int64_t cols,
+                      int64_t hidden, float eps, const void *gate, const void *up, const void *down, int group, int activation, int eight_bit, void *scratch,
+                      size_t scratch_bytes, void *sum_out, int64_t lds, void *y, int64_t ldy);
 
 /*
  * Algorithm 2, inner repeat: `steps` Adam updates (Section 5.1: learning rate lr0, multiplied

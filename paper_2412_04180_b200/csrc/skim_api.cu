@@ -799,6 +799,59 @@ int skim_add_rmsnorm(skim_ctx *ctx, const void *x, int64_t ldx, const void *resi
     return skim_launch_add_rmsnorm(ctx, n);
 }
 
+namespace {
+struct FeedForwardScratch {
+    size_t rows, scale, hidden, bytes;       // offsets
+};
+FeedForwardScratch feed_forward_scratch(int64_t tokens, int64_t cols, int64_t hidden)
+{
+    FeedForwardScratch s;
+    auto rows_of = [](int64_t n) { return (n + 15) / 16 * 16; };        // rows at whole 16-byte pieces
+    s.rows = 0;
+    s.scale = skim_align256((size_t)tokens * (size_t)rows_of(cols) * 2);
+    s.hidden = s.scale + skim_align256((size_t)tokens * 4);
+    s.bytes = s.hidden + skim_align256((size_t)tokens * (size_t)rows_of(hidden) * 2);
+    return s;
+}
+bool feed_forward_shape(int64_t tokens, int64_t cols, int64_t hidden)
+{
+    return tokens >= 0 && tokens <= SKIM_MAX_TOKENS && cols >= 1 && cols <= SKIM_MAX_GROUPED_COLS && hidden >= 1 && hidden <= SKIM_MAX_GROUPED_COLS;
+}
+}  // namespace
+
+int skim_feed_forward_bytes(int64_t tokens, int64_t cols, int64_t hidden, size_t *out)
+{
+    if (!out) return SKIM_ERR_NULL;
+    if (!feed_forward_shape(tokens, cols, hidden)) return SKIM_ERR_SHAPE;
+    *out = feed_forward_scratch(tokens, cols, hidden).bytes;
+    return SKIM_OK;
+}
+
+int skim_feed_forward(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int type, int64_t tokens, int64_t cols,
+                      int64_t hidden, float eps, const void *gate, const void *up, const void *down, int group, int activation, int eight_bit, void *scratch,
+                      size_t scratch_bytes, void *sum_out, int64_t lds, void *y, int64_t ldy)
+{
+    // what the second and the third call would refuse is refused before the first one runs
+    if (!ctx || (tokens != 0 && (!x || !gate || !up || !down || !scratch || !y))) return SKIM_ERR_NULL;
+    if ((type != SKIM_TYPE_F16 && type != SKIM_TYPE_BF16) || (activation != SKIM_ACT_SILU && activation != SKIM_ACT_GELU)) return SKIM_ERR_TYPE;
+    if (!feed_forward_shape(tokens, cols, hidden) || ldy < cols) return SKIM_ERR_SHAPE;
+    int rc = check_grouped(gate, hidden, cols, group);
+    if (!rc) rc = check_grouped(up, hidden, cols, group);
+    if (!rc) rc = check_grouped(down, cols, hidden, group);
+    if (rc) return rc;
+    if (!aligned_for(y, type)) return SKIM_ERR_ALIGN;
+    const FeedForwardScratch s = feed_forward_scratch(tokens, cols, hidden);
+    if (!ctx->ws || (reinterpret_cast<uintptr_t>(scratch) & 255u) || scratch_bytes < s.bytes) return SKIM_ERR_WORKSPACE;
+    unsigned char *base = static_cast<unsigned char *>(scratch);
+    float *scale = eight_bit ? reinterpret_cast<float *>(base + s.scale) : nullptr;
+    const int64_t ld_rows = (cols + 15) / 16 * 16, ld_hidden = (hidden + 15) / 16 * 16;
+    const int rows_type = eight_bit ? SKIM_TYPE_I8 : type;
+    rc = skim_add_rmsnorm(ctx, x, ldx, residual, ldr, weight, type, tokens, cols, eps, sum_out, lds, base + s.rows, rows_type, ld_rows, scale);
+    if (!rc) rc = skim_grouped_gated(ctx, gate, up, hidden, cols, group, activation, base + s.rows, rows_type, ld_rows, scale, tokens, base + s.hidden, type, ld_hidden);
+    if (!rc) rc = skim_grouped_matvec(ctx, down, cols, hidden, group, base + s.hidden, type, ld_hidden, nullptr, tokens, y, type, ldy);
+    return rc;
+}
+
 const char *skim_strerror(int code)
 {
     switch (code) {

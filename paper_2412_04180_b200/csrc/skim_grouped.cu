@@ -6,7 +6,7 @@
 //
 // Rounding to whole numbers is decided as by exact quotients: x / s in binary32 with correct rounding never lands on a border k + 1/2 that the exact quotient
 // misses (k + 1/2 has 5 bits, s 11, x 24, so x - (k + 1/2) s is zero or at least 2^-23 of x, more than the half unit that the rounding can move).  The
-// kernel multiplies by 1 / s instead and divides only where the product comes within 2^-15 of a border.
+// kernel multiplies by 1 / s instead and divides only where the quotient comes within 2^-15 of a border, or of the limits of the codes.
 //
 // Both kernels stream: weights (and importances) in, half a byte a weight out, or the other way round.  A thread has one row's four runs of eight
 // columns of a record, so the group's extremes are two shuffles within a quad, its 16 bytes of codes leave in one store, and a row's error
@@ -31,15 +31,18 @@ struct QuantArgs {
     unsigned long long *status;
 };
 
-__device__ __forceinline__ float rint_of_quotient(float x, float s, float by, bool &near)
+// Least and greatest of the eight values of four words and of `low`, `high`; NaN where there is one.
+__device__ __forceinline__ void extremes(const uint32_t raw[4], __half2 &low, __half2 &high)
 {
-    const float t = x * by, r = rintf(t);
-    near |= fabsf(t - r) > 0.5f - 0x1p-15f;
-    return r;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        low = __hmin2_nan(low, bits_half2(raw[u]));
+        high = __hmax2_nan(high, bits_half2(raw[u]));
+    }
 }
 
 template <int PER, bool SCALED, bool ERR>
-__global__ void __launch_bounds__(QT) skim_grouped_quantize_kernel(QuantArgs a)
+__global__ void __launch_bounds__(QT, 2) skim_grouped_quantize_kernel(QuantArgs a)
 {
     __shared__ float sums[QW][8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, p = lane & 3;
@@ -86,27 +89,36 @@ __global__ void __launch_bounds__(QT) skim_grouped_quantize_kernel(QuantArgs a)
                 }
             }
         }
-        float x[4][8], low[PER], high[PER];
+        // the clustered value of element e of run t
+        auto value = [&](int t, int e) {
+            const float w = __half2float(__ushort_as_half((unsigned short)(raw[t][e / 2] >> (16 * (e & 1)))));
+            if (!SCALED) return w;
+            const int64_t j = first + 32 * t + e;
+            return __fmul_rn(w, j < a.cols ? a.r[j] : 0.0f);
+        };
+        float low[PER], high[PER];
 #pragma unroll
-        for (int k = 0; k < PER; ++k) low[k] = high[k] = 0.0f;
+        for (int k = 0; k < PER; ++k) {
+            __half2 lo = bits_half2(0u), hi = bits_half2(0u);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int k = t * PER / 4;
+            for (int t = k * 4 / PER; t < (k + 1) * 4 / PER; ++t) extremes(raw[t], lo, hi);
+            const float l = __low2float(lo), m = __high2float(lo), n = __low2float(hi), o = __high2float(hi);
+            bad |= !(l >= -65504.0f && m >= -65504.0f && n <= 65504.0f && o <= 65504.0f);
+            low[k] = fminf(l, m);
+            high[k] = fmaxf(n, o);
+            if (SCALED) {
+                low[k] = high[k] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t h = (raw[t][e / 2] >> (16 * (e & 1))) & 0xffffu;
-                bad |= (h & 0x7c00u) == 0x7c00u;
-                x[t][e] = __half2float(__ushort_as_half((unsigned short)h));
-                if (SCALED) {
-                    const int64_t j = first + 32 * t + e;
-                    x[t][e] = __fmul_rn(x[t][e], j < a.cols ? a.r[j] : 0.0f);
-                }
-                low[k] = fminf(low[k], x[t][e]);
-                high[k] = fmaxf(high[k], x[t][e]);
+                for (int t = k * 4 / PER; t < (k + 1) * 4 / PER; ++t)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = value(t, e);
+                        low[k] = fminf(low[k], x);
+                        high[k] = fmaxf(high[k], x);
+                    }
             }
         }
-        uint32_t meta[PER];
-        float s[PER], by[PER], z[PER];
+        uint32_t meta[PER], word[4];
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
 #pragma unroll
@@ -115,37 +127,51 @@ __global__ void __launch_bounds__(QT) skim_grouped_quantize_kernel(QuantArgs a)
                 high[k] = fmaxf(high[k], __shfl_xor_sync(0xffffffffu, high[k], off));
             }
             const __half h = __float2half_rn(__fdiv_rn(__fsub_rn(high[k], low[k]), 15.0f));
-            s[k] = __half2float(h);
-            const bool some = s[k] > 0.0f;
-            bad |= !(s[k] <= 65504.0f);                      // scaled values may leave the range
-            by[k] = some ? __frcp_rn(s[k]) : 0.0f;           // no scale: every quotient, code and zero point is 0
-            z[k] = some ? fminf(rintf(__fdiv_rn(-low[k], s[k])), 15.0f) : 0.0f;
-            meta[k] = (uint32_t)__half_as_ushort(h) | (uint32_t)(int)z[k] << 16;
-        }
-        uint32_t word[4];
+            const float s = __half2float(h);
+            const bool some = s > 0.0f;
+            bad |= !(s <= 65504.0f);                         // scaled values may leave the range
+            const float by = some ? __frcp_rn(s) : 0.0f;     // no scale: every quotient, code and zero point is 0
+            const float z = some ? fminf(rintf(__fdiv_rn(-low[k], s)), 15.0f) : 0.0f;
+            const float least = -z, most = some ? 15.0f - z : 0.0f, as_code = z + 8388608.0f, border = s * (0.5f - 0x1p-15f);
+            meta[k] = (uint32_t)__half_as_ushort(h) | (uint32_t)(int)z << 16;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int k = t * PER / 4;
-            float q[8];
-            bool near = false;
+            for (int t = k * 4 / PER; t < (k + 1) * 4 / PER; ++t) {
+                // code - z is the quotient's whole number (by way of 1.5 * 2^23) within its limits, which keeps what is left of x at hand: that is the
+                // error, and says whether the quotient came near a border
+                uint32_t codes = 0x05000000u;                // less what the eight binary32 images add
+                float left[8], far = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) q[e] = rint_of_quotient(x[t][e], s[k], by[k], near);
-            if (near && s[k] > 0.0f) {
+                for (int e = 0; e < 8; ++e) {
+                    const float x = value(t, e), q = fminf(fmaxf(__fadd_rn(__fmaf_rn(x, by, 12582912.0f), -12582912.0f), least), most);
+                    left[e] = __fmaf_rn(-q, s, x);
+                    far = fmaxf(far, fabsf(left[e]));
+                    codes += __float_as_uint(q + as_code) << (4 * nibble_of(e));
+                }
+                if (far > border && some) {
+                    codes = 0x05000000u;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) q[e] = rintf(__fdiv_rn(x[t][e], s[k]));
-            }
-            word[t] = 0u;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float code = fminf(fmaxf(q[e] + z[k], 0.0f), 15.0f);
-                word[t] |= (__float_as_uint(code + 8388608.0f) & 15u) << (4 * nibble_of(e));
+                    for (int e = 0; e < 8; ++e) {
+                        const float x = value(t, e), q = fminf(fmaxf(rintf(__fdiv_rn(x, s)), least), most);
+                        left[e] = __fmaf_rn(-q, s, x);
+                        codes += __float_as_uint(q + as_code) << (4 * nibble_of(e));
+                    }
+                }
+                word[t] = codes;
                 if (ERR) {
-                    const float d = __fsub_rn(x[t][e], (code - z[k]) * s[k]);
                     if (Gr) {
-                        bad_g |= !(g[t][e] >= 0.0f && g[t][e] <= 3.402823466e38f);
-                        err = fmaf(d * d, g[t][e], err);
+                        uint32_t top = 0u;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            top = max(top, __float_as_uint(g[t][e]));
+                            err = fmaf(left[e] * left[e], g[t][e], err);
+                        }
+                        if (top >= 0x7f800000u) {            // infinite, NaN or negative, or a negative zero among the others
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) bad_g |= !(g[t][e] >= 0.0f && g[t][e] <= 3.402823466e38f);
+                        }
                     } else {
-                        err = fmaf(d, d, err);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) err = fmaf(left[e], left[e], err);
                     }
                 }
             }

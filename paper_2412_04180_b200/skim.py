@@ -28,7 +28,7 @@ EXPORTS = ["skim_create", "skim_destroy", "skim_max_cols", "skim_workspace_bytes
            "skim_quantize_matrix_host", "skim_get_status", "skim_launch_count", "skim_kernel_timing",
            "skim_kernel_times", "skim_early_exit", "skim_lloyd_iterations", "skim_strerror",
            "skim_grouped_bytes", "skim_grouped_quantize", "skim_grouped_dequantize", "skim_grouped_matvec", "skim_grouped_gated",
-           "skim_add_rmsnorm"]
+           "skim_add_rmsnorm", "skim_feed_forward_bytes", "skim_feed_forward"]
 
 # element types and activations of the products with grouped weights and of the norm
 TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2, torch.int8: 3}
@@ -65,6 +65,8 @@ def lib():
         _lib.skim_grouped_dequantize.argtypes = [vp, vp, i64, i64, i32, vp, i64]
         _lib.skim_grouped_matvec.argtypes = [vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, i64]
         _lib.skim_grouped_gated.argtypes = [vp, vp, vp, i64, i64, i32, i32, vp, i32, i64, vp, i64, vp, i32, i64]
+        _lib.skim_feed_forward_bytes.argtypes = [i64, i64, i64, vp]
+        _lib.skim_feed_forward.argtypes = [vp, vp, i64, vp, i64, vp, i32, i64, i64, i64, C.c_float, vp, vp, vp, i32, i32, i32, vp, C.c_size_t, vp, i64, vp, i64]
         _lib.skim_add_rmsnorm.argtypes = [vp, vp, i64, vp, i64, vp, i32, i64, i64, C.c_float, vp, i64, vp, i32, i64, vp]
     return _lib
 
@@ -377,7 +379,8 @@ class Skim:
             if got != rows or ldg != ld:
                 raise TypeError("importance: expected the shape and the strides of W")
         if out is None:
-            out = dict(tiles=self._new((self.grouped_bytes(rows, cols, group),), torch.uint8), rows=rows, cols=cols, group=group,
+            n = -(-rows // 16) * -(-cols // 128) * (1024 + 8192 // group) if group in (32, 64, 128) else self.grouped_bytes(rows, cols, group)
+            out = dict(tiles=self._new((n,), torch.uint8), rows=rows, cols=cols, group=group,
                        err=self._new((rows,), torch.float32) if want_err else None)
         tiles, *held = self._tiles(out, "out")
         if held != [rows, cols, group]:
@@ -451,12 +454,42 @@ class Skim:
                                     None if out_scale is None else self._plain(out_scale, "out_scale", torch.float32, rows)), "skim_add_rmsnorm")
         return out, out_scale, sum_out
 
-    def feed_forward(self, x, weight, gate, up, down, eps=1e-5, residual=None, activation="silu", eight_bit=True, out=None):
+    @staticmethod
+    def feed_forward_bytes(tokens, cols, hidden):
+        out = C.c_size_t()
+        _chk(lib().skim_feed_forward_bytes(tokens, cols, hidden, C.byref(out)), "skim_feed_forward_bytes")
+        return out.value
+
+    def feed_forward(self, x, weight, gate, up, down, eps=1e-5, residual=None, activation="silu", eight_bit=True, out=None, sum_out=None, scratch=None):
         """The feed-forward half of a decoder layer: add_rmsnorm (to 8 bits, or to x's dtype), grouped_gated, grouped_matvec.  Returns (down's
-        product in x's dtype, the new residual stream or None); ``gate`` and ``up`` are [hidden, cols], ``down`` [cols, hidden]."""
-        rows, scale, stream = self.add_rmsnorm(x, weight, eps=eps, residual=residual, out_dtype=torch.int8 if eight_bit else None)
-        hidden = self.grouped_gated(gate, up, rows, x_scale=scale, activation=activation, out_dtype=x.dtype)
-        return self.grouped_matvec(down, hidden, out=out, out_dtype=x.dtype), stream
+        product in x's dtype, the new residual stream or None); ``gate`` and ``up`` are [hidden, cols], ``down`` [cols, hidden].  ``scratch``: uint8, at
+        least feed_forward_bytes (made here if not given)."""
+        tokens, ldx = self._rows_of(x, "x", (torch.float16, torch.bfloat16))
+        kind = x.dtype
+        g, hidden, cols, group = self._tiles(gate, "gate")
+        u, *held = self._tiles(up, "up")
+        d, *back = self._tiles(down, "down")
+        if held != [hidden, cols, group] or back != [cols, hidden, group] or x.size(-1) != cols:
+            raise TypeError(f"x has {x.size(-1)} columns; rows, cols, group are {[hidden, cols, group]} in gate, {held} in up, {back} in down")
+        out, y, ldy = self._out_rows(out, kind, x, tokens, cols)
+        ldr = lds = 0
+        if residual is not None:
+            got, ldr = self._rows_of(residual, "residual", (kind,), cols)
+            if got != tokens:
+                raise TypeError(f"residual: expected {tokens} rows, got {got}")
+            if sum_out is None:
+                sum_out = self._new(x.shape, kind)
+        if sum_out is not None:
+            got, lds = self._rows_of(sum_out, "sum_out", (kind,), cols)
+            if got != tokens:
+                raise TypeError(f"sum_out: expected {tokens} rows, got {got}")
+        if scratch is None:
+            scratch = self._new((self.feed_forward_bytes(tokens, cols, hidden),), torch.uint8)
+        _chk(lib().skim_feed_forward(self._h, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
+                                     None if weight is None else self._plain(weight, "weight", kind, cols), TYPES[kind], tokens, cols, hidden, eps, g, u, d, group,
+                                     ACTIVATIONS.get(activation, -1), 1 if eight_bit else 0, self._plain(scratch, "scratch", torch.uint8, scratch.numel()),
+                                     scratch.numel(), None if sum_out is None else sum_out.data_ptr(), lds, y, ldy), "skim_feed_forward")
+        return out, sum_out
 
     def scale_update(self, W, importance, labels, alpha, steps=120, lr0=0.01, decay=0.5, decay_every=40,
                      want_trace=True):

@@ -143,5 +143,27 @@ def test_norm_refusals(lib, handle):
         assert f(**bad) == ALIGN
 
 
+def test_feed_forward_refusals(lib, handle):
+    h = handle[0]
+    n = C.c_size_t()
+    assert lib.skim_feed_forward_bytes(3, 100, 50, C.byref(n)) == 0 and n.value == 768 + 256 + 512
+    assert lib.skim_feed_forward_bytes(3, 100, 50, None) == NULL and lib.skim_feed_forward_bytes(3, 0, 50, C.byref(n)) == SHAPE
+    assert lib.skim_feed_forward_bytes(1048561, 100, 50, C.byref(n)) == SHAPE and lib.skim_feed_forward_bytes(3, 100, 131073, C.byref(n)) == SHAPE
+
+    def f(ctx=h, x=A, ldx=100, r=None, ldr=0, w=None, kind=0, tokens=3, cols=100, hidden=50, eps=1e-5, gate=A, up=A, down=A, group=32, act=0, eight=1, scratch=A,
+          size=1 << 20, s=None, lds=0, y=A, ldy=100):
+        return lib.skim_feed_forward(ctx, x, ldx, r, ldr, w, kind, tokens, cols, hidden, eps, gate, up, down, group, act, eight, scratch, size, s, lds, y, ldy)
+
+    assert f() == WORKSPACE
+    for bad in (dict(ctx=None), dict(x=None), dict(gate=None), dict(up=None), dict(down=None), dict(scratch=None), dict(y=None)):
+        assert f(**bad) == NULL
+    for bad in (dict(tokens=-1), dict(cols=0), dict(hidden=0), dict(hidden=131073), dict(ldy=99)):
+        assert f(**bad) == SHAPE
+    for bad in (dict(kind=2), dict(kind=3), dict(act=2), dict(group=48)):
+        assert f(**bad) == TYPE
+    for bad in (dict(gate=A + 8), dict(up=A + 8), dict(down=A + 8), dict(y=A + 1)):
+        assert f(**bad) == ALIGN
+
+
 def test_every_refusal_has_words(lib):
     assert b"type" in lib.skim_strerror(TYPE)
