@@ -26,19 +26,22 @@ __device__ __forceinline__ uint32_t bits_of(float v)
     return BF16 ? (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(v)) : (uint32_t)__half_as_ushort(__float2half_rn(v));
 }
 
-// Eight values from column j on; columns beyond the row are zeros.
-template <bool BF16, bool VEC>
-__device__ __forceinline__ void load8(const uint16_t *row, int64_t j, int64_t cols, float v[8])
+// Eight neighbours as they lie in memory, from column j on; columns beyond the row are zeros.
+template <bool VEC>
+__device__ __forceinline__ uint4 load8(const uint16_t *row, int64_t j, int64_t cols)
 {
-    if (VEC) {
-        const uint4 u = *reinterpret_cast<const uint4 *>(row + j);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    if (VEC) return *reinterpret_cast<const uint4 *>(row + j);
+    uint32_t h[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = value_of<BF16>((w[e / 2] >> (16 * (e & 1))) & 0xffffu);
-    } else {
+    for (int e = 0; e < 8; ++e) h[e] = j + e < cols ? (uint32_t)row[j + e] : 0u;
+    return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+}
+template <bool BF16>
+__device__ __forceinline__ void values8(uint4 u, float v[8])
+{
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = j + e < cols ? value_of<BF16>(row[j + e]) : 0.0f;
-    }
+    for (int e = 0; e < 8; ++e) v[e] = value_of<BF16>((w[e / 2] >> (16 * (e & 1))) & 0xffffu);
 }
 template <bool BF16, bool VEC>
 __device__ __forceinline__ void store8(uint16_t *row, int64_t j, int64_t cols, const float v[8])
@@ -65,117 +68,130 @@ __device__ __forceinline__ int code_of(float p, float a, float by)
     return r == r ? (int)fminf(fmaxf(r, -127.0f), 127.0f) : 0;
 }
 
-// NV pieces of eight columns a thread, in registers; NV = 0: as many as the row takes, read again for the result.
+// NV pieces of eight columns a thread, in registers; NV = 0: as many as the row takes, read again for the result.  A block goes from row to row, the next row's
+// values on their way while the warps exchange this one's sums (2048 x 8192: a block for every row 29.3 us).
 template <bool BF16, bool VEC, int NV>
-__global__ void __launch_bounds__(MAX_T) skim_add_rmsnorm_kernel(SkimNorm n)
+__global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel(SkimNorm n)
 {
-    __shared__ float sums[32], tops[32];
+    __shared__ float sums[2][32], tops[2][32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-    const int64_t row = blockIdx.x;
     skim_wait_for_previous_kernel();
     skim_let_next_kernel_start();
-    const uint16_t *xr = static_cast<const uint16_t *>(n.x) + row * n.ldx;
-    const uint16_t *rr = n.residual ? static_cast<const uint16_t *>(n.residual) + row * n.ldr : nullptr;
     const uint16_t *wr = static_cast<const uint16_t *>(n.weight);
-    uint16_t *sr = n.sum_out ? static_cast<uint16_t *>(n.sum_out) + row * n.lds : nullptr;
     const int64_t step = (int64_t)blockDim.x * 8;
-    auto sum8 = [&](int64_t j, float h[8]) {
-        load8<BF16, VEC>(xr, j, n.cols, h);
-        if (rr) {
-            float r[8];
-            load8<BF16, VEC>(rr, j, n.cols, r);
+    auto x_of = [&](int64_t row) { return static_cast<const uint16_t *>(n.x) + row * n.ldx; };
+    auto r_of = [&](int64_t row) { return static_cast<const uint16_t *>(n.residual) + row * n.ldr; };
+    auto sum8 = [&](uint4 x, uint4 r, float h[8]) {
+        values8<BF16>(x, h);
+        if (n.residual) {
+            float v[8];
+            values8<BF16>(r, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] += r[e];
+            for (int e = 0; e < 8; ++e) h[e] += v[e];
         }
     };
     auto weighted8 = [&](int64_t j, const float h[8], float p[8]) {
-        if (wr) load8<BF16, VEC>(wr, j, n.cols, p);
+        if (wr) values8<BF16>(load8<VEC>(wr, j, n.cols), p);
 #pragma unroll
         for (int e = 0; e < 8; ++e) p[e] = wr ? h[e] * p[e] : h[e];
     };
-    float sq = 0.0f, top = 0.0f;
-    float p[NV ? NV : 1][8];
-    if (NV) {
-        float h[NV ? NV : 1][8];
+    auto take8 = [&](const float h[8], const float p[8], float &sq, float &top) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t j = v * step + tid * 8;
-            if (j < n.cols) sum8(j, h[v]);
+        for (int e = 0; e < 8; ++e) {
+            sq = fmaf(h[e], h[e], sq);
+            top = fmaxf(top, fabsf(p[e]));
         }
+    };
+    constexpr int M = NV ? NV : 1;
+    uint4 xs[M], rs[M];
+    auto ask = [&](int64_t row) {
 #pragma unroll
         for (int v = 0; v < NV; ++v) {
             const int64_t j = v * step + tid * 8;
             if (j >= n.cols) break;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sq = fmaf(h[v][e], h[v][e], sq);
-            weighted8(j, h[v], p[v]);
-            if (sr) store8<BF16, VEC>(sr, j, n.cols, h[v]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(p[v][e]));
-        }
-    } else {
-        for (int64_t j = tid * 8; j < n.cols; j += step) {
-            float h[8];
-            sum8(j, h);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sq = fmaf(h[e], h[e], sq);
-            weighted8(j, h, p[0]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(p[0][e]));
-        }
-    }
-#pragma unroll
-    for (int off = 16; off; off >>= 1) {
-        sq += __shfl_xor_sync(0xffffffffu, sq, off);
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    }
-    if (lane == 0) {
-        sums[warp] = sq;
-        tops[warp] = top;
-    }
-    __syncthreads();
-    sq = lane < warps ? sums[lane] : 0.0f;
-    top = lane < warps ? tops[lane] : 0.0f;
-#pragma unroll
-    for (int off = 16; off; off >>= 1) {
-        sq += __shfl_xor_sync(0xffffffffu, sq, off);
-        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    }
-    const float rstd = 1.0f / sqrtf(sq / (float)n.cols + n.eps);
-    const float by = top > 0.0f ? 127.0f / top : 0.0f;
-    if (n.out_scale && tid == 0) n.out_scale[row] = top * rstd / 127.0f;
-    auto result8 = [&](int64_t j, float v[8]) {
-        if (n.out_type == SKIM_TYPE_I8) {
-            int8_t *o = static_cast<int8_t *>(n.out) + row * n.ldo;
-            uint32_t w[2] = {0u, 0u};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(code_of(v[e], top, by) & 255) << (8 * (e & 3));
-            if (VEC) {
-                *reinterpret_cast<uint2 *>(o + j) = make_uint2(w[0], w[1]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (j + e < n.cols) o[j + e] = (int8_t)(w[e / 4] >> (8 * (e & 3)));
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= rstd;
-            store8<BF16, VEC>(static_cast<uint16_t *>(n.out) + row * n.ldo, j, n.cols, v);
+            xs[v] = load8<VEC>(x_of(row), j, n.cols);
+            if (n.residual) rs[v] = load8<VEC>(r_of(row), j, n.cols);
         }
     };
-    if (NV) {
+    int turn = 0;
+    if (NV) ask(blockIdx.x);
+    for (int64_t row = blockIdx.x; row < n.rows; row += gridDim.x, turn ^= 1) {
+        uint16_t *sr = n.sum_out ? static_cast<uint16_t *>(n.sum_out) + row * n.lds : nullptr;
+        float sq = 0.0f, top = 0.0f;
+        float p[M][8];
+        if (NV) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t j = v * step + tid * 8;
-            if (j < n.cols) result8(j, p[v]);
+            for (int v = 0; v < NV; ++v) {
+                const int64_t j = v * step + tid * 8;
+                if (j >= n.cols) break;
+                float h[8];
+                sum8(xs[v], rs[v], h);
+                weighted8(j, h, p[v]);
+                if (sr) store8<BF16, VEC>(sr, j, n.cols, h);
+                take8(h, p[v], sq, top);
+            }
+            if (row + gridDim.x < n.rows) ask(row + gridDim.x);
+        } else {
+            for (int64_t j = tid * 8; j < n.cols; j += step) {
+                float h[8];
+                sum8(load8<VEC>(x_of(row), j, n.cols), n.residual ? load8<VEC>(r_of(row), j, n.cols) : make_uint4(0u, 0u, 0u, 0u), h);
+                weighted8(j, h, p[0]);
+                take8(h, p[0], sq, top);
+            }
         }
-    } else {
-        for (int64_t j = tid * 8; j < n.cols; j += step) {
-            float h[8];
-            sum8(j, h);
-            weighted8(j, h, p[0]);
-            if (sr) store8<BF16, VEC>(sr, j, n.cols, h);
-            result8(j, p[0]);
+#pragma unroll
+        for (int off = 16; off; off >>= 1) {
+            sq += __shfl_xor_sync(0xffffffffu, sq, off);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        }
+        if (lane == 0) {
+            sums[turn][warp] = sq;
+            tops[turn][warp] = top;
+        }
+        __syncthreads();                                     // (the next row's sums go to the other places: one barrier a row)
+        sq = lane < warps ? sums[turn][lane] : 0.0f;
+        top = lane < warps ? tops[turn][lane] : 0.0f;
+#pragma unroll
+        for (int off = 16; off; off >>= 1) {
+            sq += __shfl_xor_sync(0xffffffffu, sq, off);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        }
+        const float rstd = 1.0f / sqrtf(sq / (float)n.cols + n.eps);
+        const float by = top > 0.0f ? 127.0f / top : 0.0f;
+        if (n.out_scale && tid == 0) n.out_scale[row] = top * rstd / 127.0f;
+        auto result8 = [&](int64_t j, float v[8]) {
+            if (n.out_type == SKIM_TYPE_I8) {
+                int8_t *o = static_cast<int8_t *>(n.out) + row * n.ldo;
+                uint32_t w[2] = {0u, 0u};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w[e / 4] |= (uint32_t)(code_of(v[e], top, by) & 255) << (8 * (e & 3));
+                if (VEC) {
+                    *reinterpret_cast<uint2 *>(o + j) = make_uint2(w[0], w[1]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (j + e < n.cols) o[j + e] = (int8_t)(w[e / 4] >> (8 * (e & 3)));
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= rstd;
+                store8<BF16, VEC>(static_cast<uint16_t *>(n.out) + row * n.ldo, j, n.cols, v);
+            }
+        };
+        if (NV) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int64_t j = v * step + tid * 8;
+                if (j < n.cols) result8(j, p[v]);
+            }
+        } else {
+            for (int64_t j = tid * 8; j < n.cols; j += step) {
+                float h[8];
+                sum8(load8<VEC>(x_of(row), j, n.cols), n.residual ? load8<VEC>(r_of(row), j, n.cols) : make_uint4(0u, 0u, 0u, 0u), h);
+                weighted8(j, h, p[0]);
+                if (sr) store8<BF16, VEC>(sr, j, n.cols, h);
+                result8(j, p[0]);
+            }
         }
     }
 }
@@ -183,14 +199,15 @@ __global__ void __launch_bounds__(MAX_T) skim_add_rmsnorm_kernel(SkimNorm n)
 template <bool BF16, bool VEC>
 int launch(skim_ctx *ctx, const SkimNorm &n)
 {
-    // a warp for every 256 columns; from 2048 columns on more pieces a thread where rows are many
+    // a warp for every 256 columns; from 2048 columns on more pieces a thread where rows are many.  Many rows are dealt to as many blocks as the SMs hold.
     const int64_t pieces = (n.cols + 7) / 8;
     int nv = 1;
-    while (nv < 4 && (pieces > (int64_t)nv * MAX_T || (n.rows > ctx->sm_count && pieces >= (int64_t)nv * 512))) nv *= 2;
-    if (pieces > (int64_t)nv * MAX_T) nv = 0;
+    while (nv < 4 && (pieces > (int64_t)nv * MAX_T || (n.rows > ctx->sm_count && pieces >= (int64_t)nv * 256))) nv *= 2;
+    if (pieces > (nv == 4 ? 4 * 512 : nv * MAX_T)) nv = 0;
     const int64_t threads = nv ? (pieces + nv - 1) / nv : MAX_T;
     const unsigned block = (unsigned)((threads + 31) / 32 * 32);
-    const dim3 grid((unsigned)n.rows);
+    const int64_t held = (int64_t)ctx->sm_count * (block <= 64 ? 16 : nv == 4 ? (512 / block > 0 ? 512 / block : 1) : 1024 / block);
+    const dim3 grid((unsigned)(nv && n.rows > held ? held : n.rows));
     switch (nv) {
     case 1: return skim_launch_dependent(ctx, skim_add_rmsnorm_kernel<BF16, VEC, 1>, grid, block, 0, n);
     case 2: return skim_launch_dependent(ctx, skim_add_rmsnorm_kernel<BF16, VEC, 2>, grid, block, 0, n);

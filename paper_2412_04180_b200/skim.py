@@ -33,6 +33,8 @@ EXPORTS = ["skim_create", "skim_destroy", "skim_max_cols", "skim_workspace_bytes
 # element types and activations of the products with grouped weights and of the norm
 TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2, torch.int8: 3}
 ACTIVATIONS = {"silu": 0, "gelu": 1}
+TOKEN_TYPES = (torch.float16, torch.bfloat16, torch.int8)
+STREAM_TYPES = (torch.float16, torch.bfloat16)
 
 
 class SkimError(RuntimeError):
@@ -103,6 +105,7 @@ class Skim:
 
     def __init__(self, device=0, stream=None, rows=0, cols=0):
         self.device = torch.device("cuda", device)
+        self._index = device
         self._stream = stream
         handle = C.c_void_p()
         sp = C.c_void_p(stream.cuda_stream if stream is not None else 0)
@@ -314,40 +317,49 @@ class Skim:
 
     # ---- weights of 4 bits with group scales, their products with token rows, and the norm in front of them
     # (The calls that a decoded token makes are bound by the host: their checks ask a tensor for as little as they can.)
-    def _new(self, shape, dtype):
+    def _new(self, dtype, *shape):
         """A tensor of the context's device, made on the context's stream (which writes it)."""
         if self._stream is None or torch.cuda.current_stream(self.device).cuda_stream == self._stream.cuda_stream:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return torch.empty(*shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self._stream):
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return torch.empty(*shape, dtype=dtype, device=self.device)
 
     def _rows_of(self, t, name, dtypes, cols=None):
-        """(rows, stride in elements) of a matrix, or of a vector as one row; elements of a row lie side by side."""
-        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.dtype not in dtypes:
+        """(rows, columns, stride in elements) of a matrix, or of a vector as one row; elements of a row lie side by side."""
+        if not isinstance(t, torch.Tensor) or t.get_device() != self._index or t.dtype not in dtypes:
             raise TypeError(f"{name}: expected a tensor on {self.device} of dtype {' or '.join(str(d) for d in dtypes)}")
-        n = t.dim()
-        if not 1 <= n <= 2 or (cols is not None and t.size(-1) != cols):
-            raise TypeError(f"{name}: expected a vector or a matrix" + ("" if cols is None else f" of {cols} columns") + f", got shape {tuple(t.shape)}")
-        if t.stride(-1) != 1 and t.size(-1) > 1:
+        shape, strides = t.shape, t.stride()
+        if len(shape) == 2:
+            rows, n = shape
+            ld, one = strides
+        elif len(shape) == 1:
+            rows, n, ld, one = 1, shape[0], 0, strides[0]
+        else:
+            rows = n = ld = one = -1
+        if rows < 0 or (cols is not None and n != cols):
+            raise TypeError(f"{name}: expected a vector or a matrix" + ("" if cols is None else f" of {cols} columns") + f", got shape {tuple(shape)}")
+        if one != 1 and n > 1:
             raise TypeError(f"{name}: the elements of a row have to lie side by side")
-        if n == 2:
-            rows = t.size(0)
-            if rows > 1:
-                return rows, t.stride(0)
-            return rows, t.size(1)
-        return 1, t.size(0)
+        return rows, n, ld if rows > 1 else n
+
+    def _like(self, t, name, kind, rows, cols):
+        """Pointer and stride of a matrix, or a vector, with as many rows and columns as another."""
+        got, _, ld = self._rows_of(t, name, (kind,), cols)
+        if got != rows:
+            raise TypeError(f"{name}: expected {rows} rows, got {got}")
+        return t.data_ptr(), ld
 
     def _plain(self, t, name, dtype, n):
-        if not (isinstance(t, torch.Tensor) and t.get_device() == self.device.index and t.dtype is dtype and t.is_contiguous() and t.numel() == n):
+        if not (isinstance(t, torch.Tensor) and t.get_device() == self._index and t.dtype is dtype and t.is_contiguous() and t.numel() == n):
             raise TypeError(f"{name}: expected a contiguous tensor on {self.device} of dtype {dtype} with {n} elements")
         return t.data_ptr()
 
     def _out_rows(self, out, dtype, x, rows, n):
         """The result [x's rows, n] (a vector where x is one), its pointer and its stride."""
         if out is None:
-            out = self._new((n,) if x.dim() == 1 else (rows, n), dtype)
+            out = self._new(dtype, n) if x.dim() == 1 else self._new(dtype, rows, n)
             return out, out.data_ptr(), n
-        got, ld = self._rows_of(out, "out", (dtype,), n)
+        got, _, ld = self._rows_of(out, "out", (dtype,), n)
         if got != rows or out.dim() != x.dim():
             raise TypeError(f"out: expected {rows} rows of {n} elements, like x, got shape {tuple(out.shape)}")
         return out, out.data_ptr(), ld
@@ -360,7 +372,7 @@ class Skim:
 
     def _tiles(self, q, name):
         t, rows, cols, group = q["tiles"], q["rows"], q["cols"], q["group"]
-        if t.get_device() != self.device.index or t.dtype is not torch.uint8 or not t.is_contiguous():
+        if t.get_device() != self._index or t.dtype is not torch.uint8 or not t.is_contiguous():
             raise TypeError(f"{name}: expected contiguous uint8 tiles on {self.device}")
         if group not in (32, 64, 128) or t.numel() < -(-rows // 16) * -(-cols // 128) * (1024 + 8192 // group):
             raise TypeError(f"{name}: {t.numel()} bytes of tiles do not hold {rows} x {cols} weights in groups of {group}")
@@ -370,23 +382,21 @@ class Skim:
         """Uniform 4-bit codes with a scale and a zero point per ``group`` (32, 64 or 128) columns of the float16 matrix W (of W / alpha
         where a scale vector is installed).  Returns dict(tiles uint8, rows, cols, group, err): the stored form, which grouped_dequantize, grouped_matvec
         and grouped_gated read, and (want_err) the float32 [rows] error, weighted with ``importance`` (float32, like W), else None."""
-        rows, ld = self._rows_of(W, "W", (torch.float16,))
-        cols = W.shape[-1]
+        rows, cols, ld = self._rows_of(W, "W", (torch.float16,))
         if W.dim() != 2:
             raise TypeError(f"W: expected a matrix, got shape {tuple(W.shape)}")
         if importance is not None:
-            got, ldg = self._rows_of(importance, "importance", (torch.float32,), cols)
+            got, _, ldg = self._rows_of(importance, "importance", (torch.float32,), cols)
             if got != rows or ldg != ld:
                 raise TypeError("importance: expected the shape and the strides of W")
         if out is None:
             n = -(-rows // 16) * -(-cols // 128) * (1024 + 8192 // group) if group in (32, 64, 128) else self.grouped_bytes(rows, cols, group)
-            out = dict(tiles=self._new((n,), torch.uint8), rows=rows, cols=cols, group=group,
-                       err=self._new((rows,), torch.float32) if want_err else None)
+            out = dict(tiles=self._new(torch.uint8, n), rows=rows, cols=cols, group=group, err=self._new(torch.float32, rows) if want_err else None)
         tiles, *held = self._tiles(out, "out")
         if held != [rows, cols, group]:
             raise TypeError(f"out: holds rows, cols, group {held}, expected {[rows, cols, group]}")
         err = out.get("err")
-        _chk(lib().skim_grouped_quantize(self._h, W.data_ptr(), None if importance is None else importance.data_ptr(), rows, cols, ld, group, tiles,
+        _chk((_lib or lib()).skim_grouped_quantize(self._h, W.data_ptr(), None if importance is None else importance.data_ptr(), rows, cols, ld, group, tiles,
                                          None if err is None else self._plain(err, "err", torch.float32, rows)), "skim_grouped_quantize")
         return out
 
@@ -394,15 +404,15 @@ class Skim:
         """float16 [rows, cols] values of a grouped_quantize() result."""
         tiles, rows, cols, group = self._tiles(q, "q")
         if out is None:
-            out = self._new((rows, cols), torch.float16)
-        got, ld = self._rows_of(out, "out", (torch.float16,), cols)
-        if got != rows:
-            raise TypeError(f"out: expected {rows} rows, got {got}")
-        _chk(lib().skim_grouped_dequantize(self._h, tiles, rows, cols, group, out.data_ptr(), ld), "skim_grouped_dequantize")
+            out = self._new(torch.float16, rows, cols)
+            y, ld = out.data_ptr(), cols
+        else:
+            y, ld = self._like(out, "out", torch.float16, rows, cols)
+        _chk((_lib or lib()).skim_grouped_dequantize(self._h, tiles, rows, cols, group, y, ld), "skim_grouped_dequantize")
         return out
 
     def _tokens(self, x, x_scale, cols):
-        tokens, ldx = self._rows_of(x, "x", (torch.float16, torch.bfloat16, torch.int8), cols)
+        tokens, _, ldx = self._rows_of(x, "x", TOKEN_TYPES, cols)
         return tokens, ldx, TYPES[x.dtype], None if x_scale is None else self._plain(x_scale, "x_scale", torch.float32, tokens)
 
     def grouped_matvec(self, q, x, x_scale=None, out=None, out_dtype=torch.float32):
@@ -427,30 +437,31 @@ class Skim:
                                       tokens, y, TYPES.get(out.dtype, -1), ldy), "skim_grouped_gated")
         return out
 
+    def _residual(self, x, kind, rows, cols, residual, sum_out):
+        """(sum_out, made where there is a residual; pointer and stride of the residual; of sum_out)"""
+        r = t = None
+        ldr = lds = 0
+        if residual is not None:
+            r, ldr = self._like(residual, "residual", kind, rows, cols)
+            if sum_out is None:
+                sum_out = self._new(kind, *x.shape)
+                return sum_out, r, ldr, sum_out.data_ptr(), cols
+        if sum_out is not None:
+            t, lds = self._like(sum_out, "sum_out", kind, rows, cols)
+        return sum_out, r, ldr, t, lds
+
     def add_rmsnorm(self, x, weight=None, eps=1e-5, residual=None, out_dtype=None, out=None, out_scale=None, sum_out=None):
         """The root-mean-square norm of x + residual, times ``weight`` [cols].  Returns (out, out_scale, sum): out in x's dtype (float16 or
         bfloat16) with out_scale None, or, out_dtype torch.int8, codes with out_scale float32 [rows]; sum is x + residual, the new residual stream, or
         None without a residual (unless sum_out is given).  sum_out may be residual or x itself."""
-        dtypes = (torch.float16, torch.bfloat16)
-        rows, ldx = self._rows_of(x, "x", dtypes)
-        cols, kind = x.shape[-1], x.dtype
+        rows, cols, ldx = self._rows_of(x, "x", STREAM_TYPES)
+        kind = x.dtype
         out, y, ldo = self._out_rows(out, (out_dtype or kind) if out is None else out.dtype, x, rows, cols)
-        ldr = lds = 0
-        if residual is not None:
-            got, ldr = self._rows_of(residual, "residual", (kind,), cols)
-            if got != rows:
-                raise TypeError(f"residual: expected {rows} rows, got {got}")
-            if sum_out is None:
-                sum_out = self._new(x.shape, kind)
-        if sum_out is not None:
-            got, lds = self._rows_of(sum_out, "sum_out", (kind,), cols)
-            if got != rows:
-                raise TypeError(f"sum_out: expected {rows} rows, got {got}")
+        sum_out, r, ldr, t, lds = self._residual(x, kind, rows, cols, residual, sum_out)
         if out.dtype == torch.int8 and out_scale is None:
-            out_scale = self._new((rows,), torch.float32)
-        _chk((_lib or lib()).skim_add_rmsnorm(self._h, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
-                                    None if weight is None else self._plain(weight, "weight", kind, cols), TYPES[kind], rows, cols, eps,
-                                    None if sum_out is None else sum_out.data_ptr(), lds, y, TYPES.get(out.dtype, -1), ldo,
+            out_scale = self._new(torch.float32, rows)
+        _chk((_lib or lib()).skim_add_rmsnorm(self._h, x.data_ptr(), ldx, r, ldr, None if weight is None else self._plain(weight, "weight", kind, cols),
+                                    TYPES[kind], rows, cols, eps, t, lds, y, TYPES.get(out.dtype, -1), ldo,
                                     None if out_scale is None else self._plain(out_scale, "out_scale", torch.float32, rows)), "skim_add_rmsnorm")
         return out, out_scale, sum_out
 
@@ -464,31 +475,21 @@ class Skim:
         """The feed-forward half of a decoder layer: add_rmsnorm (to 8 bits, or to x's dtype), grouped_gated, grouped_matvec.  Returns (down's
         product in x's dtype, the new residual stream or None); ``gate`` and ``up`` are [hidden, cols], ``down`` [cols, hidden].  ``scratch``: uint8, at
         least feed_forward_bytes (made here if not given)."""
-        tokens, ldx = self._rows_of(x, "x", (torch.float16, torch.bfloat16))
+        tokens, width, ldx = self._rows_of(x, "x", STREAM_TYPES)
         kind = x.dtype
         g, hidden, cols, group = self._tiles(gate, "gate")
         u, *held = self._tiles(up, "up")
         d, *back = self._tiles(down, "down")
-        if held != [hidden, cols, group] or back != [cols, hidden, group] or x.size(-1) != cols:
-            raise TypeError(f"x has {x.size(-1)} columns; rows, cols, group are {[hidden, cols, group]} in gate, {held} in up, {back} in down")
+        if held != [hidden, cols, group] or back != [cols, hidden, group] or width != cols:
+            raise TypeError(f"x has {width} columns; rows, cols, group are {[hidden, cols, group]} in gate, {held} in up, {back} in down")
         out, y, ldy = self._out_rows(out, kind, x, tokens, cols)
-        ldr = lds = 0
-        if residual is not None:
-            got, ldr = self._rows_of(residual, "residual", (kind,), cols)
-            if got != tokens:
-                raise TypeError(f"residual: expected {tokens} rows, got {got}")
-            if sum_out is None:
-                sum_out = self._new(x.shape, kind)
-        if sum_out is not None:
-            got, lds = self._rows_of(sum_out, "sum_out", (kind,), cols)
-            if got != tokens:
-                raise TypeError(f"sum_out: expected {tokens} rows, got {got}")
+        sum_out, r, ldr, t, lds = self._residual(x, kind, tokens, cols, residual, sum_out)
         if scratch is None:
-            scratch = self._new((self.feed_forward_bytes(tokens, cols, hidden),), torch.uint8)
-        _chk(lib().skim_feed_forward(self._h, x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr,
+            scratch = self._new(torch.uint8, self.feed_forward_bytes(tokens, cols, hidden))
+        _chk((_lib or lib()).skim_feed_forward(self._h, x.data_ptr(), ldx, r, ldr,
                                      None if weight is None else self._plain(weight, "weight", kind, cols), TYPES[kind], tokens, cols, hidden, eps, g, u, d, group,
                                      ACTIVATIONS.get(activation, -1), 1 if eight_bit else 0, self._plain(scratch, "scratch", torch.uint8, scratch.numel()),
-                                     scratch.numel(), None if sum_out is None else sum_out.data_ptr(), lds, y, ldy), "skim_feed_forward")
+                                     scratch.numel(), t, lds, y, ldy), "skim_feed_forward")
         return out, sum_out
 
     def scale_update(self, W, importance, labels, alpha, steps=120, lr0=0.01, decay=0.5, decay_every=40,
