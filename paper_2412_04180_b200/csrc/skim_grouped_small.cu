@@ -36,7 +36,7 @@ template <int XT, int PER, int NREC, int NT>
 struct Ring {
     static constexpr int NW = NREC == 1 ? 8 : 4, T = NW * 32, BLOCKS = NREC == 1 ? 2 : NT == 1 || XT == SKIM_TYPE_I8 ? 5 : 3;
     static constexpr int SETS = NREC == 1 && NT * (XT == SKIM_TYPE_I8 ? 1 : 2) <= 2 ? 3 : 2;
-    static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, DEPTH = NREC == 1 ? 6 : 4, PLACE = NREC * RECORD, BYTES = DEPTH * PLACE;
+    static constexpr int RECORD = SKIM_RECORD_CODES + 64 * PER, DEPTH = SETS == 3 ? 3 : 4, PLACE = NREC * RECORD, BYTES = DEPTH * PLACE;
     static_assert(DEPTH % SETS == 0, "a place goes with a set");
 };
 
@@ -326,7 +326,7 @@ int launch(skim_ctx *ctx, const SmallArgs &all)
     const int64_t blocks = (a.rt * a.kw + NW - 1) / NW;
     if (blocks * a.split > 0x7fffffff) return SKIM_ERR_SHAPE;
     auto kernel = skim_grouped_small_kernel<XT, PER, NREC, NT>;
-    if (smem > 47 * 1024) SKIM_CUDA_OK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    static_assert(smem <= 47 * 1024, "no permission needed");
     constexpr int64_t most = 65535 * (8 * NT);               // tokens of a launch
     for (int64_t first = 0; first < all.p.tokens; first += most) {
         a.p.x = static_cast<const unsigned char *>(all.p.x) + first * all.p.ldx * (XT == SKIM_TYPE_I8 ? 1 : 2);

@@ -299,6 +299,42 @@ def test_many_tokens(ctx, rows, cols, tokens, pad, runs, dtype, group):
         assert np.all(np.abs(as_np(ctx.grouped_gated(qs[0], qs[1], x, x_scale=xs, activation="gelu", out_dtype=torch.bfloat16).double()) - want) <= gated)
 
 
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_many_tokens_not_finite_and_the_rows_between(ctx, dtype):
+    rows, cols, tokens = 3001, 520, 700
+    q = ctx.grouped_quantize(torch.from_numpy(weights(rows, cols)).cuda(), 128)
+    x, _, _ = token_rows(tokens, cols, dtype, pad=8)
+    room = torch.full((tokens + 1, rows + 3), 5.0, device="cuda")
+    clean = ctx.grouped_matvec(q, x)
+    gate = ctx.grouped_gated(q, q, x)
+    x[1, 7], x[600, 519] = float("nan"), float("-inf")
+    y = ctx.grouped_matvec(q, x, out=room[:tokens, :rows])
+    keep = [t for t in range(tokens) if t not in (1, 600)]
+    assert torch.equal(y[keep], clean[keep]) and bool(y[1].isnan().all()) and not bool(y[600].isfinite().any())
+    assert torch.equal(ctx.grouped_gated(q, q, x)[keep], gate[keep])
+    assert bool((room[:, rows:] == 5).all()) and bool((room[tokens] == 5).all())
+
+
+def test_rows_far_apart(ctx):
+    """Rows of x and of y, and of the norm, more than 2^31 elements from the first one."""
+    cols, rows, far = 256, 48, (1 << 30) + 64
+    room = torch.empty(3 * far, dtype=torch.float16, device="cuda")
+    x = room.view(3, far)[:, :cols]
+    near, xv, _ = token_rows(3, cols, torch.float16)
+    x.copy_(near)
+    q, _ = held(weights(rows, cols), 64)
+    y = room.view(3, far)[:, 512:512 + rows]
+    ctx.grouped_matvec(q, x, out=y)
+    assert torch.equal(y, ctx.grouped_matvec(q, near, out_dtype=torch.float16))
+    out = room.view(3, far)[:, 1024:1024 + cols]
+    ctx.add_rmsnorm(x, residual=x, out=out)
+    assert torch.equal(out, ctx.add_rmsnorm(near, residual=near)[0])
+    W = room.view(3, far)[:, 2048:2048 + cols]
+    w = torch.from_numpy(weights(3, cols)).cuda()
+    W.copy_(w)
+    assert torch.equal(ctx.grouped_quantize(W, 32)["tiles"], ctx.grouped_quantize(w, 32)["tiles"])
+
+
 def test_a_vector_and_one_row_are_the_same_and_runs_repeat(ctx):
     q, _ = held(weights(70, 700), 64)
     x, _, _ = token_rows(1, 700, torch.float16)
@@ -460,7 +496,7 @@ def test_captured_and_replayed_on_a_stream_of_its_own(skimlib):
     w = torch.ones(cols, dtype=torch.float16, device="cuda")
     graphs = []
     torch.cuda.synchronize()
-    for tokens in (2, 70):
+    for tokens in (2, 70, 1500):
         x, r = norm_rows(tokens, cols, torch.float16, 1), norm_rows(tokens, cols, torch.float16, 2)
         with torch.cuda.stream(s):
             c.feed_forward(x, w, gate, up, down, residual=r)
