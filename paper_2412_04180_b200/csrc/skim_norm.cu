@@ -105,21 +105,23 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
     constexpr int M = NV ? NV : 1;
     uint4 xs[M], rs[M];
     auto ask = [&](int64_t row) {
+        if constexpr (NV != 0) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int64_t j = v * step + tid * 8;
-            if (j >= n.cols) break;
-            xs[v] = load8<VEC>(x_of(row), j, n.cols);
-            if (n.residual) rs[v] = load8<VEC>(r_of(row), j, n.cols);
+            for (int v = 0; v < NV; ++v) {
+                const int64_t j = v * step + tid * 8;
+                if (j >= n.cols) break;
+                xs[v] = load8<VEC>(x_of(row), j, n.cols);
+                if (n.residual) rs[v] = load8<VEC>(r_of(row), j, n.cols);
+            }
         }
     };
     int turn = 0;
-    if (NV) ask(blockIdx.x);
+    ask(blockIdx.x);
     for (int64_t row = blockIdx.x; row < n.rows; row += gridDim.x, turn ^= 1) {
         uint16_t *sr = n.sum_out ? static_cast<uint16_t *>(n.sum_out) + row * n.lds : nullptr;
         float sq = 0.0f, top = 0.0f;
         float p[M][8];
-        if (NV) {
+        if constexpr (NV != 0) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int64_t j = v * step + tid * 8;
@@ -178,7 +180,7 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
                 store8<BF16, VEC>(static_cast<uint16_t *>(n.out) + row * n.ldo, j, n.cols, v);
             }
         };
-        if (NV) {
+        if constexpr (NV != 0) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
                 const int64_t j = v * step + tid * 8;
