@@ -338,13 +338,17 @@ int skim_grouped_dequantize(skim_ctx *ctx, const void *tiles, int64_t rows, int6
  * skim_grouped_gated: y = act(gate x) * (up x), both matrices [rows][cols] in the stored form with the same group size, in one kernel.
  *
  * rows, tokens >= 0 (0 is a no-op), 1 <= cols <= SKIM_MAX_GROUPED_COLS.  ldx >= cols, ldy >= rows.  Matrices are 16-byte aligned; x and y need the
- * alignment of their elements only (rows of x at multiples of 16 bytes -- 8 for 8-bit rows -- are faster).  y must not overlap x.
+ * alignment of their elements only.  y must not overlap x.
+ *   scratch  device, 16-byte aligned, or NULL: where it has the bytes that skim_grouped_scratch_bytes names (host-only; 0 where it would not help), rows of x that
+ *            do not lie at multiples of 16 bytes are copied there first, which many tokens are much faster for.  Calls in flight do not share it.
  * Needs a workspace of 512 bytes (status word: SKIM_STATUS_TIMEOUT).  Same inputs, same bits, on every run.
  */
+int skim_grouped_scratch_bytes(const skim_ctx *ctx, int64_t rows, int64_t cols, int group, int gated, const void *x, int x_type, int64_t ldx,
+                               int64_t tokens, size_t *out);
 int skim_grouped_matvec(skim_ctx *ctx, const void *tiles, int64_t rows, int64_t cols, int group, const void *x, int x_type, int64_t ldx,
-                        const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy);
-int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t rows, int64_t cols, int group, int activation,
-                       const void *x, int x_type, int64_t ldx, const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy);
+                        const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy, void *scratch, size_t scratch_bytes);
+int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t rows, int64_t cols, int group, int activation, const void *x, int x_type,
+                       int64_t ldx, const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy, void *scratch, size_t scratch_bytes);
 
 /*
  * The residual's addition and the root-mean-square norm of token rows:

@@ -692,7 +692,24 @@ int check_grouped(const void *tiles, int64_t rows, int64_t cols, int group)
 unsigned type_bytes(int type) { return type == SKIM_TYPE_F32 ? 4u : type == SKIM_TYPE_I8 ? 1u : 2u; }
 bool aligned_for(const void *p, int type) { return reinterpret_cast<uintptr_t>(p) % type_bytes(type) == 0; }
 
-int grouped_product(skim_ctx *ctx, const SkimGroupedProduct &p)
+// Bytes of a copy of the token rows at whole 16-byte pieces, 0 where the call is no faster with one.  The copy is worth its launch where it opens the way to the
+// tensor-memory kernel, or where the other one would read many pieces element by element (us, rows at odd addresses without it and with it: 4096 x 4096, 16 fp16 tokens
+// 15.0 and 9.5; 300 tokens 218 and 26; 4096 x 11008, 8 8-bit tokens 22.9 and 11.5).
+size_t aligned_copy_bytes(const skim_ctx *ctx, const SkimGroupedProduct &p)
+{
+    const int64_t bytes = p.x_type == SKIM_TYPE_I8 ? 1 : 2, ld = skim_aligned_stride(p.cols, p.x_type);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(p.x) | (uintptr_t)(p.ldx * bytes);
+    if (p.tokens < 2 || p.rows == 0 || (at & 15u) == 0) return 0;
+    SkimGroupedProduct copy = p;
+    copy.x = nullptr;                                        // an aligned address
+    copy.ldx = ld;
+    const bool pieces = (at & (8 * bytes - 1)) == 0;         // the few-token kernel can read whole pieces as it is
+    const int64_t records = skim_record_tiles(p.rows, SKIM_RECORD_ROWS) * skim_record_tiles(p.cols, SKIM_RECORD_COLS) * (p.gated ? 2 : 1);
+    if (skim_grouped_gemm_takes(ctx, copy) || (!pieces && records * p.tokens >= 16384)) return (size_t)p.tokens * (size_t)ld * (size_t)bytes;
+    return 0;
+}
+
+int grouped_product(skim_ctx *ctx, const SkimGroupedProduct &p, void *scratch, size_t scratch_bytes)
 {
     const bool none = p.rows == 0 || p.tokens == 0;           // empty arrays may have no address
     if (!ctx || (!none && (!p.tiles[0] || (p.gated && !p.tiles[1]) || !p.x || !p.out))) return SKIM_ERR_NULL;
@@ -704,12 +721,19 @@ int grouped_product(skim_ctx *ctx, const SkimGroupedProduct &p)
     if (rc) return rc;
     if (p.tokens < 0 || p.tokens > SKIM_MAX_TOKENS || p.ldx < p.cols || p.ldo < p.rows) return SKIM_ERR_SHAPE;
     if (!aligned_for(p.x, p.x_type) || !aligned_for(p.out, p.out_type) || !aligned_for(p.x_scale, SKIM_TYPE_F32)) return SKIM_ERR_ALIGN;
-    if (!ctx->ws) return SKIM_ERR_WORKSPACE;
+    if (!ctx->ws || (reinterpret_cast<uintptr_t>(scratch) & 15u)) return SKIM_ERR_WORKSPACE;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return SKIM_ERR_CUDA;
     SkimGroupedProduct q = p;
     q.status = (unsigned long long *)ctx->ws;
     if (none) return SKIM_OK;
+    const size_t copy = scratch ? aligned_copy_bytes(ctx, p) : 0;
+    if (copy && copy <= scratch_bytes) {
+        rc = skim_launch_align_rows(ctx, q, scratch);
+        if (rc) return rc;
+        q.x = scratch;
+        q.ldx = skim_aligned_stride(p.cols, p.x_type);
+    }
     return skim_grouped_gemm_takes(ctx, q) ? skim_launch_grouped_gemm(ctx, q) : skim_launch_grouped_small(ctx, q);
 }
 
@@ -752,19 +776,34 @@ int skim_grouped_dequantize(skim_ctx *ctx, const void *tiles, int64_t rows, int6
     return skim_launch_grouped_dequantize(ctx, static_cast<const unsigned char *>(tiles), rows, cols, group, out, ld_out);
 }
 
+int skim_grouped_scratch_bytes(const skim_ctx *ctx, int64_t rows, int64_t cols, int group, int gated, const void *x, int x_type, int64_t ldx, int64_t tokens, size_t *out)
+{
+    if (!ctx || !out) return SKIM_ERR_NULL;
+    if (x_type != SKIM_TYPE_F16 && x_type != SKIM_TYPE_BF16 && x_type != SKIM_TYPE_I8) return SKIM_ERR_TYPE;
+    const int rc = check_grouped(nullptr, rows, cols, group);
+    if (rc) return rc;
+    if (tokens < 0 || tokens > SKIM_MAX_TOKENS || ldx < cols) return SKIM_ERR_SHAPE;
+    SkimGroupedProduct p = {};
+    p.gated = gated ? 1 : 0;
+    p.rows = rows; p.cols = cols; p.group = group;
+    p.x = x; p.x_type = x_type; p.ldx = ldx; p.tokens = tokens;
+    *out = aligned_copy_bytes(ctx, p);
+    return SKIM_OK;
+}
+
 int skim_grouped_matvec(skim_ctx *ctx, const void *tiles, int64_t rows, int64_t cols, int group, const void *x, int x_type, int64_t ldx,
-                        const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy)
+                        const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy, void *scratch, size_t scratch_bytes)
 {
     SkimGroupedProduct p = {};
     p.tiles[0] = static_cast<const unsigned char *>(tiles);
     p.rows = rows; p.cols = cols; p.group = group;
     p.x = x; p.x_type = x_type; p.ldx = ldx; p.x_scale = x_scale; p.tokens = tokens;
     p.out = y; p.out_type = y_type; p.ldo = ldy;
-    return grouped_product(ctx, p);
+    return grouped_product(ctx, p, scratch, scratch_bytes);
 }
 
-int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t rows, int64_t cols, int group, int activation,
-                       const void *x, int x_type, int64_t ldx, const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy)
+int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t rows, int64_t cols, int group, int activation, const void *x, int x_type,
+                       int64_t ldx, const float *x_scale, int64_t tokens, void *y, int y_type, int64_t ldy, void *scratch, size_t scratch_bytes)
 {
     SkimGroupedProduct p = {};
     p.tiles[0] = static_cast<const unsigned char *>(gate);
@@ -773,7 +812,7 @@ int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t 
     p.rows = rows; p.cols = cols; p.group = group;
     p.x = x; p.x_type = x_type; p.ldx = ldx; p.x_scale = x_scale; p.tokens = tokens;
     p.out = y; p.out_type = y_type; p.ldo = ldy;
-    return grouped_product(ctx, p);
+    return grouped_product(ctx, p, scratch, scratch_bytes);
 }
 
 int skim_add_rmsnorm(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int type, int64_t rows,
@@ -847,8 +886,8 @@ int skim_feed_forward(skim_ctx *ctx, const void *x, int64_t ldx, const void *res
     const int64_t ld_rows = (cols + 15) / 16 * 16, ld_hidden = (hidden + 15) / 16 * 16;
     const int rows_type = eight_bit ? SKIM_TYPE_I8 : type;
     rc = skim_add_rmsnorm(ctx, x, ldx, residual, ldr, weight, type, tokens, cols, eps, sum_out, lds, base + s.rows, rows_type, ld_rows, scale);
-    if (!rc) rc = skim_grouped_gated(ctx, gate, up, hidden, cols, group, activation, base + s.rows, rows_type, ld_rows, scale, tokens, base + s.hidden, type, ld_hidden);
-    if (!rc) rc = skim_grouped_matvec(ctx, down, cols, hidden, group, base + s.hidden, type, ld_hidden, nullptr, tokens, y, type, ldy);
+    if (!rc) rc = skim_grouped_gated(ctx, gate, up, hidden, cols, group, activation, base + s.rows, rows_type, ld_rows, scale, tokens, base + s.hidden, type, ld_hidden, nullptr, 0);
+    if (!rc) rc = skim_grouped_matvec(ctx, down, cols, hidden, group, base + s.hidden, type, ld_hidden, nullptr, tokens, y, type, ldy, nullptr, 0);
     return rc;
 }
 

@@ -268,6 +268,26 @@ __global__ void __launch_bounds__(DT) skim_grouped_dequantize_kernel(BackArgs a)
     }
 }
 
+// ---------------------------------------------------------------- token rows at any address, copied to whole 16-byte pieces
+
+// A block has a token; a thread moves words of the copy, so a warp's loads lie side by side.
+template <typename E>
+__global__ void __launch_bounds__(256) skim_align_rows_kernel(const E *x, int64_t ldx, int cols, uint32_t *out, int words)
+{
+    constexpr int N = 4 / sizeof(E);
+    const int64_t token = blockIdx.x;
+    skim_wait_for_previous_kernel();
+    skim_let_next_kernel_start();
+    const E *row = x + token * ldx;
+    for (int w = threadIdx.x; w < words; w += 256) {
+        uint32_t v = 0u;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (w * N + e < cols) v |= (uint32_t)row[w * N + e] << (8 * sizeof(E) * e);
+        out[token * words + w] = v;
+    }
+}
+
 }  // namespace
 
 int skim_launch_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *importance, const float *rscale, int64_t rows, int64_t cols, int64_t ld, int group,
@@ -313,4 +333,18 @@ int skim_launch_grouped_dequantize(skim_ctx *ctx, const unsigned char *tiles, in
     case 2: return skim_launch_dependent(ctx, skim_grouped_dequantize_kernel<2>, grid, DT, 0, a);
     default: return skim_launch_dependent(ctx, skim_grouped_dequantize_kernel<4>, grid, DT, 0, a);
     }
+}
+
+// Elements between rows of the copy.
+int64_t skim_aligned_stride(int64_t cols, int x_type)
+{
+    const int64_t piece = x_type == SKIM_TYPE_I8 ? 16 : 8;
+    return (cols + piece - 1) / piece * piece;
+}
+int skim_launch_align_rows(skim_ctx *ctx, const SkimGroupedProduct &p, void *scratch)
+{
+    const int bytes = p.x_type == SKIM_TYPE_I8 ? 1 : 2, words = (int)(skim_aligned_stride(p.cols, p.x_type) * bytes / 4);
+    const dim3 grid((unsigned)p.tokens);
+    if (bytes == 1) return skim_launch_dependent(ctx, skim_align_rows_kernel<uint8_t>, grid, 256, 0, static_cast<const uint8_t *>(p.x), p.ldx, (int)p.cols, static_cast<uint32_t *>(scratch), words);
+    return skim_launch_dependent(ctx, skim_align_rows_kernel<uint16_t>, grid, 256, 0, static_cast<const uint16_t *>(p.x), p.ldx, (int)p.cols, static_cast<uint32_t *>(scratch), words);
 }

@@ -173,6 +173,8 @@ struct SkimGroupedProduct {
 };
 bool skim_grouped_gemm_takes(const skim_ctx *ctx, const SkimGroupedProduct &p);
 int skim_launch_grouped_gemm(skim_ctx *ctx, const SkimGroupedProduct &p);
+int64_t skim_aligned_stride(int64_t cols, int x_type);
+int skim_launch_align_rows(skim_ctx *ctx, const SkimGroupedProduct &p, void *scratch);
 int skim_launch_grouped_small(skim_ctx *ctx, const SkimGroupedProduct &p);
 int skim_launch_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *importance, const float *rscale, int64_t rows, int64_t cols, int64_t ld, int group,
                                  unsigned char *tiles, float *err);

@@ -262,43 +262,76 @@ __global__ void __launch_bounds__(Ring<XT, PER, NREC, NT>::T, Ring<XT, PER, NREC
     for (int r = 0; r < NREC; ++r)
 #pragma unroll
         for (int n = 0; n < NT; ++n) *reinterpret_cast<float4 *>(sums + (r * NT + n) * 128 + lane * 4) = make_float4(total[r][n][0], total[r][n][1], total[r][n][2], total[r][n][3]);
-    if (a.split > 1) cluster_barrier();
-    else __syncthreads();
-    // each block of the cluster finishes a share of the rows; 16 threads have the rows of a tile
-    const int outs = rows_of_block * 16 * tokens, share = (outs / 16 + a.split - 1) / a.split * 16;
-    const int end = share * (rank + 1) < outs ? share * (rank + 1) : outs;
-    for (int e = share * rank + (int)threadIdx.x; e < end; e += T) {
-        const int i = e & 15, in_block = (e >> 4) & (rows_of_block - 1), t = (e >> 4) / rows_of_block;
-        const int64_t row = ((int64_t)block * rows_of_block + in_block) * SKIM_RECORD_ROWS + i;
-        if (row >= a.p.rows) continue;
-        const int64_t token = t0 + t;
-        const unsigned char *at = smem + in_block * a.kw * R::BYTES + ((t >> 3) * 128 + ((i & 7) * 4 + ((t & 7) >> 1)) * 4 + (i >> 3) * 2 + (t & 1)) * 4;
-        float v = 0.0f, up = 0.0f;
-        for (int s = 0; s < a.split; ++s)
-            for (int w = 0; w < a.kw; ++w) {
-                const float *one = reinterpret_cast<const float *>(at + w * R::BYTES), *two = one + (NREC - 1) * NT * 128;
-                v += s == rank ? *one : load_from_rank(one, s);
-                if (NREC == 2) up += s == rank ? *two : load_from_rank(two, s);
-            }
+    __syncthreads();
+    // an output's place among a warp's totals: 16 threads have the rows of a tile
+    const int outs = rows_of_block * 16 * tokens;
+    auto place_of = [&](int e, int &in_block, int &t) {
+        const int i = e & 15;
+        in_block = (e >> 4) & (rows_of_block - 1);
+        t = (e >> 4) / rows_of_block;
+        return reinterpret_cast<float *>(smem + in_block * a.kw * R::BYTES) + (t >> 3) * 128 + ((i & 7) * 4 + ((t & 7) >> 1)) * 4 + (i >> 3) * 2 + (t & 1);
+    };
+    auto finish = [&](int e, int in_block, int t, float v, float up) {
+        const int64_t row = ((int64_t)block * rows_of_block + in_block) * SKIM_RECORD_ROWS + (e & 15), token = t0 + t;
+        if (row >= a.p.rows) return;
         if (a.p.x_scale) {
             const float scale = a.p.x_scale[token];
             v *= scale;
             up *= scale;
         }
         store_as(a.p.out, a.p.out_type, token * a.p.ldo + row, NREC == 2 ? activation(a.p.act, v) * up : v);
+    };
+    for (int e = threadIdx.x; e < outs; e += T) {
+        int in_block, t;
+        float *one = place_of(e, in_block, t);
+        float v = *one, up = NREC == 2 ? one[NT * 128] : 0.0f;
+#pragma unroll
+        for (int w = 1; w < NW; ++w)
+            if (w < a.kw) {
+                v += one[w * (R::BYTES / 4)];
+                if (NREC == 2) up += one[w * (R::BYTES / 4) + NT * 128];
+            }
+        if (a.split == 1) {
+            finish(e, in_block, t, v, up);
+        } else {
+            *one = v;
+            if (NREC == 2) one[NT * 128] = up;
+        }
+    }
+    if (a.split > 1) {
+        cluster_barrier();
+        // each block of the cluster finishes a share of the rows; the others' sums are on their way together
+        const int share = (outs / 16 + a.split - 1) / a.split * 16, end = share * (rank + 1) < outs ? share * (rank + 1) : outs;
+        for (int e = share * rank + (int)threadIdx.x; e < end; e += T) {
+            int in_block, t;
+            const float *one = place_of(e, in_block, t);
+            float part_v[MAX_SPLIT], part_up[MAX_SPLIT];
+#pragma unroll
+            for (int s = 0; s < MAX_SPLIT; ++s) {
+                part_v[s] = s < a.split ? load_from_rank(one, s) : 0.0f;
+                part_up[s] = NREC == 2 && s < a.split ? load_from_rank(one + NT * 128, s) : 0.0f;
+            }
+            float v = part_v[0], up = part_up[0];
+#pragma unroll
+            for (int s = 1; s < MAX_SPLIT; ++s) {
+                v += part_v[s];
+                up += part_up[s];
+            }
+            finish(e, in_block, t, v, up);
+        }
     }
     if (a.split > 1) cluster_barrier();                      // the other blocks' totals are read before they end
 }
 
-// How the warps share rows and columns, by the clocks of an SM: a warp alone takes about 350 a record (its chain of copies, expansion and products); warps
-// together share the issue slots at about 28 a record, and 60 for the start and the end of each.  A cluster's barriers and sums cost 2500: blocks share columns only
+// How the warps share rows and columns, by the clocks of an SM: a warp alone takes about 600 a record (its chain of copies, expansion and products); warps
+// together share the issue slots at about 28 a record, and 60 for the start and the end of each.  A cluster's barriers and sums cost 2500 and 100 a token (gated 300): blocks share columns only
 // where rows are few and long.  (us, kw warps a block and split blocks, measured: 4096 x 4096, one token, 4 warps: kw 4 5.5, kw 2 split 2 6.5, kw 1 split 4 6.8;
-// gated 11008 x 4096: kw 4 13.9, kw 2 15.8, kw 2 split 2 14.8.)
+// gated 11008 x 4096: kw 4 13.9, kw 2 15.8, kw 2 split 2 14.8; 128 x 11008, kw 8: alone 6.0, split 4 3.7.)
 struct Plan {
     int kw, split;
 };
-constexpr int RECORD_ALONE = 350, RECORD_SHARED = 28, WARP_ENDS = 60, CLUSTER_COST = 2500;
-Plan plan_of(const skim_ctx *ctx, int64_t rt, int ct, int nrec, int nt, int nw, int resident)
+constexpr int RECORD_ALONE = 600, RECORD_SHARED = 28, WARP_ENDS = 60, CLUSTER_COST = 2500, CLUSTER_TOKEN = 100;
+Plan plan_of(const skim_ctx *ctx, int64_t rt, int ct, int nrec, int nt, int tokens, int nw, int resident)
 {
     Plan best = {1, 1};
     int64_t least = INT64_MAX;
@@ -307,7 +340,7 @@ Plan plan_of(const skim_ctx *ctx, int64_t rt, int ct, int nrec, int nt, int nw, 
             if (kw * s > ct) break;                          // every part has a record
             const int64_t chunks = (ct + kw * s - 1) / (kw * s), blocks = (rt * kw + nw - 1) / nw * s, rounds = (blocks + ctx->sm_count - 1) / ctx->sm_count;
             const int64_t waves = (rounds + resident - 1) / resident, together = (rounds + waves - 1) / waves * nw * RECORD_SHARED;
-            const int64_t cost = waves * chunks * nrec * nt * (together > RECORD_ALONE ? together : RECORD_ALONE) + rounds * nw * WARP_ENDS + (s > 1 ? CLUSTER_COST : 0);
+            const int64_t cost = waves * chunks * nrec * (1 + nt) / 2 * (together > RECORD_ALONE ? together : RECORD_ALONE) + rounds * nw * WARP_ENDS + (s > 1 ? CLUSTER_COST + CLUSTER_TOKEN * tokens * (nrec == 1 ? 1 : 3) : 0);
             if (cost < least) best = {kw, s}, least = cost;
         }
     return best;
@@ -320,7 +353,7 @@ int launch(skim_ctx *ctx, const SmallArgs &all)
     using R = Ring<XT, PER, NREC, NT>;
     constexpr size_t smem = (size_t)R::NW * R::BYTES;
     constexpr int T = R::T, NW = R::NW;
-    const Plan plan = plan_of(ctx, a.rt, a.ct, NREC, NT, NW, NREC == 1 ? 3 : R::BLOCKS);
+    const Plan plan = plan_of(ctx, a.rt, a.ct, NREC, NT, a.p.tokens < 8 * NT ? (int)a.p.tokens : 8 * NT, NW, NREC == 1 ? 3 : R::BLOCKS);
     a.split = plan.split;
     a.kw = plan.kw;
     const int64_t blocks = (a.rt * a.kw + NW - 1) / NW;

@@ -28,7 +28,7 @@ EXPORTS = ["skim_create", "skim_destroy", "skim_max_cols", "skim_workspace_bytes
            "skim_quantize_matrix_host", "skim_get_status", "skim_launch_count", "skim_kernel_timing",
            "skim_kernel_times", "skim_early_exit", "skim_lloyd_iterations", "skim_strerror",
            "skim_grouped_bytes", "skim_grouped_quantize", "skim_grouped_dequantize", "skim_grouped_matvec", "skim_grouped_gated",
-           "skim_add_rmsnorm", "skim_feed_forward_bytes", "skim_feed_forward"]
+           "skim_grouped_scratch_bytes", "skim_add_rmsnorm", "skim_feed_forward_bytes", "skim_feed_forward"]
 
 # element types and activations of the products with grouped weights and of the norm
 TYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2, torch.int8: 3}
@@ -65,8 +65,9 @@ def lib():
         _lib.skim_grouped_bytes.argtypes = [i64, i64, i32, vp]
         _lib.skim_grouped_quantize.argtypes = [vp] * 3 + [i64, i64, i64, i32, vp, vp]
         _lib.skim_grouped_dequantize.argtypes = [vp, vp, i64, i64, i32, vp, i64]
-        _lib.skim_grouped_matvec.argtypes = [vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, i64]
-        _lib.skim_grouped_gated.argtypes = [vp, vp, vp, i64, i64, i32, i32, vp, i32, i64, vp, i64, vp, i32, i64]
+        _lib.skim_grouped_matvec.argtypes = [vp, vp, i64, i64, i32, vp, i32, i64, vp, i64, vp, i32, i64, vp, C.c_size_t]
+        _lib.skim_grouped_gated.argtypes = [vp, vp, vp, i64, i64, i32, i32, vp, i32, i64, vp, i64, vp, i32, i64, vp, C.c_size_t]
+        _lib.skim_grouped_scratch_bytes.argtypes = [vp, i64, i64, i32, i32, vp, i32, i64, i64, vp]
         _lib.skim_feed_forward_bytes.argtypes = [i64, i64, i64, vp]
         _lib.skim_feed_forward.argtypes = [vp, vp, i64, vp, i64, vp, i32, i64, i64, i64, C.c_float, vp, vp, vp, i32, i32, i32, vp, C.c_size_t, vp, i64, vp, i64]
         _lib.skim_add_rmsnorm.argtypes = [vp, vp, i64, vp, i64, vp, i32, i64, i64, C.c_float, vp, i64, vp, i32, i64, vp]
@@ -415,17 +416,31 @@ class Skim:
         tokens, _, ldx = self._rows_of(x, "x", TOKEN_TYPES, cols)
         return tokens, ldx, TYPES[x.dtype], None if x_scale is None else self._plain(x_scale, "x_scale", torch.float32, tokens)
 
-    def grouped_matvec(self, q, x, x_scale=None, out=None, out_dtype=torch.float32):
+    def _scratch(self, scratch, rows, cols, group, gated, x, kind, ldx, tokens):
+        """Pointer and bytes of the room for a copy of rows that do not lie at multiples of 16 bytes, and the tensor."""
+        if scratch is None:
+            if tokens < 2 or (x.data_ptr() | ldx * x.element_size()) & 15 == 0:
+                return None, 0, None
+            n = C.c_size_t()
+            _chk(lib().skim_grouped_scratch_bytes(self._h, rows, cols, group, gated, x.data_ptr(), kind, ldx, tokens, C.byref(n)), "skim_grouped_scratch_bytes")
+            if n.value == 0:
+                return None, 0, None
+            scratch = self._new(torch.uint8, n.value)
+        return self._plain(scratch, "scratch", torch.uint8, scratch.numel()), scratch.numel(), scratch
+
+    def grouped_matvec(self, q, x, x_scale=None, out=None, out_dtype=torch.float32, scratch=None):
         """[tokens, rows] (or [rows] for a vector x): x_scale * x Wq^T for float16, bfloat16 or int8 rows x [tokens, cols], straight from a
-        grouped_quantize() result ``q``; out_dtype is float32, float16 or bfloat16."""
+        grouped_quantize() result ``q``; out_dtype is float32, float16 or bfloat16.  scratch: uint8, room for a copy of rows that do not lie at
+        multiples of 16 bytes (made here where it helps and is not given)."""
         tiles, rows, cols, group = self._tiles(q, "q")
         tokens, ldx, kind, scale = self._tokens(x, x_scale, cols)
         out, y, ldy = self._out_rows(out, out_dtype if out is None else out.dtype, x, tokens, rows)
-        _chk((_lib or lib()).skim_grouped_matvec(self._h, tiles, rows, cols, group, x.data_ptr(), kind, ldx, scale, tokens, y, TYPES.get(out.dtype, -1), ldy),
-             "skim_grouped_matvec")
+        room, room_bytes, scratch = self._scratch(scratch, rows, cols, group, 0, x, kind, ldx, tokens) if ldx >= cols else (None, 0, None)
+        _chk((_lib or lib()).skim_grouped_matvec(self._h, tiles, rows, cols, group, x.data_ptr(), kind, ldx, scale, tokens, y, TYPES.get(out.dtype, -1), ldy,
+                                                 room, room_bytes), "skim_grouped_matvec")
         return out
 
-    def grouped_gated(self, gate, up, x, x_scale=None, activation="silu", out=None, out_dtype=torch.float32):
+    def grouped_gated(self, gate, up, x, x_scale=None, activation="silu", out=None, out_dtype=torch.float32, scratch=None):
         """act(gate x) * (up x) for two grouped_quantize() results of one shape; arguments as for grouped_matvec, activation "silu" or "gelu"."""
         tiles, rows, cols, group = self._tiles(gate, "gate")
         other, *held = self._tiles(up, "up")
@@ -433,8 +448,9 @@ class Skim:
             raise TypeError(f"up: holds rows, cols, group {held}, gate {[rows, cols, group]}")
         tokens, ldx, kind, scale = self._tokens(x, x_scale, cols)
         out, y, ldy = self._out_rows(out, out_dtype if out is None else out.dtype, x, tokens, rows)
+        room, room_bytes, scratch = self._scratch(scratch, rows, cols, group, 1, x, kind, ldx, tokens) if ldx >= cols else (None, 0, None)
         _chk((_lib or lib()).skim_grouped_gated(self._h, tiles, other, rows, cols, group, ACTIVATIONS.get(activation, -1), x.data_ptr(), kind, ldx, scale,
-                                      tokens, y, TYPES.get(out.dtype, -1), ldy), "skim_grouped_gated")
+                                                tokens, y, TYPES.get(out.dtype, -1), ldy, room, room_bytes), "skim_grouped_gated")
         return out
 
     def _residual(self, x, kind, rows, cols, residual, sum_out):

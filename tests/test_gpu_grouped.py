@@ -280,7 +280,9 @@ def test_few_rows_and_long_rows_share_the_columns(ctx):
                                                        (3001, 520, 700, 16, 2),           # ragged in every direction
                                                        (520, 4101, 300, 11, 2),           # few tiles: four pairs of blocks share the columns
                                                        (1030, 4096, 601, 0, 2),           # two pairs
-                                                       (12000, 2000, 20, 0, 2)])          # few tokens, many rows
+                                                       (12000, 2000, 20, 0, 2),           # few tokens, many rows
+                                                       (3001, 519, 700, 2, 2),            # rows at odd addresses, copied first
+                                                       (4100, 4099, 9, 0, 2)])
 def test_many_tokens(ctx, rows, cols, tokens, pad, runs, dtype, group):
     """All rows and tokens, run by run, against 64 bits (products on the GPU, of the oracle's values)."""
     w = [weights(rows, cols, seed) for seed in (1, 2)]
@@ -313,6 +315,21 @@ def test_many_tokens_not_finite_and_the_rows_between(ctx, dtype):
     assert torch.equal(y[keep], clean[keep]) and bool(y[1].isnan().all()) and not bool(y[600].isfinite().any())
     assert torch.equal(ctx.grouped_gated(q, q, x)[keep], gate[keep])
     assert bool((room[:, rows:] == 5).all()) and bool((room[tokens] == 5).all())
+
+
+def test_room_for_a_copy_given_or_too_small(ctx):
+    q = ctx.grouped_quantize(torch.from_numpy(weights(2000, 1000)).cuda(), 128)
+    x, xv, _ = token_rows(500, 1000, torch.float16, pad=3)
+    value = grouped.values(*grouped.quantize(weights(2000, 1000), 128), 128)
+    exact, size = grouped.product(value, xv)
+    bound = product_bound(1000, 128, size, exact, torch.float32)
+    for n in (500 * 1000 * 2, 500 * 1000 * 2 - 1, 0):
+        room = torch.full((n + 64,), 0xA5, dtype=torch.uint8, device="cuda")
+        y = ctx.grouped_matvec(q, x, scratch=room[:n])
+        assert np.all(np.abs(y.double().cpu().numpy() - exact) <= bound)
+        assert bool((room[n:] == 0xA5).all()) and (n == 500 * 1000 * 2 or bool((room == 0xA5).all()))
+    with pytest.raises(Exception, match="SKIM_ERR_WORKSPACE"):
+        ctx.grouped_matvec(q, x, scratch=torch.empty(2000000, dtype=torch.uint8, device="cuda")[8:])
 
 
 def test_rows_far_apart(ctx):

@@ -109,9 +109,9 @@ def test_product_refusals(lib, handle):
     h = handle[0]
 
     def both(code, ctx=h, tiles=A, rows=4, cols=64, group=32, act=0, x=A, xt=0, ldx=64, xs=None, tokens=2, y=A, yt=2, ldy=4):
-        assert lib.skim_grouped_matvec(ctx, tiles, rows, cols, group, x, xt, ldx, xs, tokens, y, yt, ldy) == code
-        assert lib.skim_grouped_gated(ctx, A, tiles, rows, cols, group, act, x, xt, ldx, xs, tokens, y, yt, ldy) == code
-        assert lib.skim_grouped_gated(ctx, tiles, A, rows, cols, group, act, x, xt, ldx, xs, tokens, y, yt, ldy) == code
+        assert lib.skim_grouped_matvec(ctx, tiles, rows, cols, group, x, xt, ldx, xs, tokens, y, yt, ldy, None, 0) == code
+        assert lib.skim_grouped_gated(ctx, A, tiles, rows, cols, group, act, x, xt, ldx, xs, tokens, y, yt, ldy, None, 0) == code
+        assert lib.skim_grouped_gated(ctx, tiles, A, rows, cols, group, act, x, xt, ldx, xs, tokens, y, yt, ldy, None, 0) == code
 
     both(WORKSPACE)
     for bad in (dict(ctx=None), dict(tiles=None), dict(x=None), dict(y=None)):
@@ -123,8 +123,21 @@ def test_product_refusals(lib, handle):
     for bad in (dict(tiles=A + 8), dict(x=A + 1), dict(xt=1, x=A + 1), dict(y=A + 2), dict(yt=0, y=A + 1), dict(xs=A + 2)):
         both(ALIGN, **bad)
     for act in (-1, 2):
-        assert lib.skim_grouped_gated(h, A, A, 4, 64, 32, act, A, 0, 64, None, 2, A, 2, 4) == TYPE
+        assert lib.skim_grouped_gated(h, A, A, 4, 64, 32, act, A, 0, 64, None, 2, A, 2, 4, None, 0) == TYPE
     both(WORKSPACE, xt=3, x=A + 1, xs=A)
+
+
+def test_scratch_bytes(lib, handle):
+    """Bytes only where rows lie at odd addresses and there is work enough."""
+    h, n = handle[0], C.c_size_t(7)
+    f = lambda *a: (lib.skim_grouped_scratch_bytes(h, *a, C.byref(n)), n.value)
+    assert f(4096, 4096, 128, 0, A, 0, 4096, 300) == (0, 0)                                # at multiples of 16 bytes
+    assert f(4096, 4096, 128, 0, A, 0, 4099, 1) == (0, 0) and f(64, 64, 32, 0, A, 0, 67, 2) == (0, 0)
+    assert f(4096, 4097, 128, 0, A, 0, 4099, 8) == (0, 8 * 4104 * 2) and f(4096, 4097, 64, 1, A + 1, 3, 4097, 8) == (0, 8 * 4112)
+    assert f(4096, 4096, 128, 0, A, 3, 4104, 8) == (0, 0)                                  # 8 bytes are enough for few 8-bit rows
+    assert lib.skim_grouped_scratch_bytes(h, 1, 1, 32, 0, A, 0, 1, 1, None) == NULL and lib.skim_grouped_scratch_bytes(None, 1, 1, 32, 0, A, 0, 1, 1, C.byref(n)) == NULL
+    assert f(4, 64, 32, 0, A, 2, 64, 1)[0] == TYPE and f(4, 64, 48, 0, A, 0, 64, 1)[0] == TYPE
+    assert f(4, 64, 32, 0, A, 0, 63, 1)[0] == SHAPE and f(4, 64, 32, 0, A, 0, 64, -1)[0] == SHAPE
 
 
 def test_norm_refusals(lib, handle):
