@@ -37,6 +37,10 @@ TOKEN_TYPES = (torch.float16, torch.bfloat16, torch.int8)
 STREAM_TYPES = (torch.float16, torch.bfloat16)
 
 
+# the current stream's handle; torch.cuda.current_stream makes an object of it every time
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class SkimError(RuntimeError):
     def __init__(self, code, where):
         self.code = code
@@ -319,10 +323,10 @@ class Skim:
     # ---- weights of 4 bits with group scales, their products with token rows, and the norm in front of them
     # (The calls that a decoded token makes are bound by the host: their checks ask a tensor for as little as they can.)
     def _new(self, dtype, *shape):
-        """A tensor of the context's device, made on the context's stream (which writes it)."""
-        if self._stream is None or torch.cuda.current_stream(self.device).cuda_stream == self._stream.cuda_stream:
+        """A tensor of the context's device, made on the context's stream (which writes it), whichever stream is the current one."""
+        if _current_stream(self._index) == (0 if self._stream is None else self._stream.cuda_stream):
             return torch.empty(*shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(self._stream):
+        with torch.cuda.stream(self._stream or torch.cuda.default_stream(self.device)):
             return torch.empty(*shape, dtype=dtype, device=self.device)
 
     def _rows_of(self, t, name, dtypes, cols=None):

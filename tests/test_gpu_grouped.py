@@ -534,6 +534,36 @@ def test_captured_and_replayed_on_a_stream_of_its_own(skimlib):
     c.close()
 
 
+def test_results_are_made_on_the_contexts_stream(ctx):
+    """Another stream is the current one: results and scratch come from the context's stream, so what was freed there is not written over early."""
+    q = ctx.grouped_quantize(torch.from_numpy(weights(2000, 1000)).cuda(), 128)
+    x, _, _ = token_rows(300, 1000, torch.float16, pad=3)
+    want = ctx.grouped_matvec(q, x)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        got = [ctx.grouped_matvec(q, x) for _ in range(8)]
+        out, scale, stream = ctx.add_rmsnorm(x, residual=x, out_dtype=torch.int8)
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want) for y in got) and torch.equal(stream, x + x)
+
+
+def test_the_most_tokens(ctx):
+    rows, cols, tokens = 33, 40, 1048560
+    w = weights(rows, cols)
+    q = ctx.grouped_quantize(torch.from_numpy(w).cuda(), 32)
+    value = torch.from_numpy(grouped.values(*grouped.quantize(w, 32), 32)).cuda()
+    x = torch.randn((tokens, cols), device="cuda").half()
+    y = ctx.grouped_matvec(q, x)
+    exact, size = x.double() @ value.t(), x.double().abs() @ value.abs().t()
+    steps = 17 * 2 + 2 + 8 + 8 + 4                         # as product_bound counts them
+    off = steps * 2.0 ** -23 * size
+    assert bool(((y.double() - exact).abs() <= off + 2.0 ** -24 * (exact.abs() + off)).all())
+    out, scale, _ = ctx.add_rmsnorm(x, out_dtype=torch.int8)
+    assert int(out.abs().amax(dim=1).amin()) == 127 and bool(scale.isfinite().all())
+    with pytest.raises(Exception, match="SKIM_ERR_SHAPE"):
+        ctx.grouped_matvec(q, torch.zeros((tokens + 1, cols), dtype=torch.float16, device="cuda"))
+
+
 def test_two_contexts_on_two_streams_at_once(skimlib):
     streams = [torch.cuda.Stream() for _ in range(2)]
     q, value = held(weights(640, 1536), 64)
