@@ -694,7 +694,7 @@ bool aligned_for(const void *p, int type) { return reinterpret_cast<uintptr_t>(p
 
 // Bytes of a copy of the token rows at whole 16-byte pieces, 0 where the call is no faster with one.  The copy is worth its launch where it opens the way to the
 // tensor-memory kernel, or where the other one would read many pieces element by element (us, rows at odd addresses without it and with it: 4096 x 4096, 16 fp16 tokens
-// 15.0 and 9.5; 300 tokens 218 and 26; 4096 x 11008, 8 8-bit tokens 22.9 and 11.5).
+// 15.0 and 8.8; 300 tokens 218 and 24.7; 4096 x 11008, 8 8-bit tokens 22.9 and 11.6).
 size_t aligned_copy_bytes(const skim_ctx *ctx, const SkimGroupedProduct &p)
 {
     const int64_t bytes = p.x_type == SKIM_TYPE_I8 ? 1 : 2, ld = skim_aligned_stride(p.cols, p.x_type);
