@@ -564,10 +564,15 @@ def test_the_most_tokens(ctx):
         ctx.grouped_matvec(q, torch.zeros((tokens + 1, cols), dtype=torch.float16, device="cuda"))
 
 
-def test_two_contexts_on_two_streams_at_once(skimlib):
-    streams = [torch.cuda.Stream() for _ in range(2)]
-    q, value = held(weights(640, 1536), 64)
-    xs = [token_rows(t, 1536, torch.bfloat16, seed=t) for t in (3, 48)]
+def test_three_contexts_on_streams_of_their_own_at_once(skimlib):
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    w = weights(3000, 1536)
+    tiles, value = held(w[:16], 64)[0], grouped.values(*grouped.quantize(w, 64), 64)
+    maker = skimlib.Skim(device=0)
+    maker.set_workspace(torch.empty(4096, dtype=torch.uint8, device="cuda"))
+    q = maker.grouped_quantize(torch.from_numpy(w).cuda(), 64)
+    assert torch.equal(q["tiles"][:tiles["tiles"].numel()], tiles["tiles"])
+    xs = [token_rows(t, 1536, torch.bfloat16, seed=t) for t in (3, 48, 500)]
     torch.cuda.synchronize()
     ctxs = [skimlib.Skim(device=0, stream=s) for s in streams]
     for c in ctxs:
