@@ -31,11 +31,14 @@ __device__ __forceinline__ uint32_t bits_of(float v)
 template <bool VEC>
 __device__ __forceinline__ uint4 load8(const uint16_t *row, int64_t j, int64_t cols)
 {
-    if (VEC) return *reinterpret_cast<const uint4 *>(row + j);
-    uint32_t h[8];
+    if constexpr (VEC) {
+        return *reinterpret_cast<const uint4 *>(row + j);
+    } else {
+        uint32_t h[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) h[e] = j + e < cols ? (uint32_t)row[j + e] : 0u;
-    return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        for (int e = 0; e < 8; ++e) h[e] = j + e < cols ? (uint32_t)row[j + e] : 0u;
+        return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+    }
 }
 template <bool BF16>
 __device__ __forceinline__ void values8(uint4 u, float v[8])
