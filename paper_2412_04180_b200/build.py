@@ -22,6 +22,14 @@ def _stale(lib=LIB) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def command(lib, defines=()) -> list:
+    """The compiler's command line for `lib`, the preprocessor's definitions among it (NAME or NAME=text without a comma)."""
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    return [nvcc, *("-D" + d for d in defines), "-std=c++17", "-O3", "--threads", "0", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
+            "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+            "-o", lib] + [os.path.join(CSRC, s) for s in SOURCES]
+
+
 def build(force: bool = False, verbose: bool = False, checked: bool = False) -> str:
     """Builds libskim.so; checked=True builds libskim_checked.so instead, in which every computed index
     into shared memory, a row record or a scratch list is range-checked (a violation sets
@@ -29,12 +37,7 @@ def build(force: bool = False, verbose: bool = False, checked: bool = False) -> 
     lib = LIB_CHECKED if checked else LIB
     if not force and not _stale(lib):
         return lib
-    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
-    cmd = [nvcc, "-std=c++17", "-O3", "--threads", "0", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
-           "-Xcompiler", "-fPIC", "-shared", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
-           "-o", lib] + [os.path.join(CSRC, s) for s in SOURCES]
-    if checked:
-        cmd.insert(1, "-DSKIM_CHECK_BOUNDS")
+    cmd = command(lib, ["SKIM_CHECK_BOUNDS"] if checked else [])
     if verbose:
         cmd.insert(1, "-Xptxas=-v")
     subprocess.run(cmd, check=True)

@@ -21,6 +21,11 @@ using namespace skimg;
 
 constexpr int MAX_SPLIT = 8;
 
+// Whether a lane may find record `done` of its warp's ring in time: a test's build lets some lanes give up where others do not.
+#ifndef SKIM_RECORD_IN_TIME
+#define SKIM_RECORD_IN_TIME true
+#endif
+
 struct SmallArgs {
     SkimGroupedProduct p;
     int ct;
@@ -239,7 +244,9 @@ __global__ void __launch_bounds__(Ring<XT, PER, NREC, NT>::T, Ring<XT, PER, NREC
                         sum_x[n][k][1] = c[1];
                     }
             }
-            if (!(ok = barrier_wait(&full[warp][d], parity))) break;
+            // for all lanes or for none: their limits may end on either side of the copy's end, and what follows is the whole warp's
+            ok = __all_sync(0xffffffffu, SKIM_RECORD_IN_TIME && barrier_wait(&full[warp][d], parity)) != 0;
+            if (!ok) break;
 #pragma unroll
             for (int r = 0; r < NREC; ++r) take_record<XT, PER, NT>(ring + d * R::PLACE + r * R::RECORD, now, sum_x, total[r]);
             read_before_copy();
