@@ -357,8 +357,8 @@ int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t 
  *   sum_out    out, may be NULL: h rounded to `type`, the new residual stream
  *   out        out, out_type == type: p * rstd, rounded once; out_type == SKIM_TYPE_I8: codes rint(127 p / a), a = max_j |p_j| of the
  *              row, decided as by the exact quotient (ties to even), standing for code * out_scale
- *   out_scale  out [rows] binary32, SKIM_TYPE_I8 only: a * rstd / 127.  A row that holds a value that is not finite gets a scale that is NaN or Inf;
- *              its codes are in range, 0 where the quotient is not a number.
+ *   out_scale  out [rows] binary32, SKIM_TYPE_I8 only: a * rstd / 127.  A row where h or p holds a value that is not finite gets a scale that is NaN or
+ *              Inf; its codes are in range, 0 where the quotient is not a number.
  * Sums of squares are binary32.  sum_out may be x or residual, and a 16-bit out may be x or residual where sum_out is not the same (same pointer and stride);
  * no other overlap.  rows >= 0 (0 is a no-op), 1 <= cols <= SKIM_MAX_GROUPED_COLS, strides (elements) >= cols, eps finite and >= 0.  No workspace is used.
  */

@@ -62,6 +62,14 @@ __device__ __forceinline__ void store8(uint16_t *row, int64_t j, int64_t cols, c
     }
 }
 
+// The greater one, NaN where either is: a maximum that drops NaN would hide it under a finite scale.
+__device__ __forceinline__ float greatest(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 // rint(127 p / a), decided as by the exact quotient: the product with 127 / a is off by less than 2^-14, and within 5e-5 of a border the quotient is
 // taken in binary64, where 127 p is exact and the rounding cannot reach a border that the exact quotient does not lie on.
 __device__ __forceinline__ int code_of(float p, float a, float by)
@@ -103,7 +111,7 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             sq = fmaf(h[e], h[e], sq);
-            top = fmaxf(top, fabsf(p[e]));
+            top = greatest(top, fabsf(p[e]));
         }
     };
     constexpr int M = NV ? NV : 1;
@@ -148,7 +156,7 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
 #pragma unroll
         for (int off = 16; off; off >>= 1) {
             sq += __shfl_xor_sync(0xffffffffu, sq, off);
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            top = greatest(top, __shfl_xor_sync(0xffffffffu, top, off));
         }
         if (lane == 0) {
             sums[turn][warp] = sq;
@@ -160,7 +168,7 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
 #pragma unroll
         for (int off = 16; off; off >>= 1) {
             sq += __shfl_xor_sync(0xffffffffu, sq, off);
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            top = greatest(top, __shfl_xor_sync(0xffffffffu, top, off));
         }
         const float rstd = 1.0f / sqrtf(sq / (float)n.cols + n.eps);
         const float by = top > 0.0f ? 127.0f / top : 0.0f;
