@@ -359,8 +359,8 @@ int skim_grouped_gated(skim_ctx *ctx, const void *gate, const void *up, int64_t 
  *              row, decided as by the exact quotient (ties to even), standing for code * out_scale
  *   out_scale  out [rows] binary32, SKIM_TYPE_I8 only: a * rstd / 127.  A row where h or p holds a value that is not finite gets a scale that is NaN or
  *              Inf; its codes are in range, 0 where the quotient is not a number.
- * Sums of squares are binary32.  sum_out may be x or residual, and a 16-bit out may be x or residual where sum_out is not the same (same pointer and stride);
- * no other overlap.  rows >= 0 (0 is a no-op), 1 <= cols <= SKIM_MAX_GROUPED_COLS, strides (elements) >= cols, eps finite and >= 0.  No workspace is used.
+ * Sums of squares are binary32, of scaled values where they would leave its range.  sum_out may be x or residual, and a 16-bit out may be x or residual
+ * where sum_out is not the same (same pointer and stride); no other overlap.  rows >= 0 (0 is a no-op), 1 <= cols <= SKIM_MAX_GROUPED_COLS, strides (elements) >= cols, eps finite and >= 0.  No workspace is used.
  */
 int skim_add_rmsnorm(skim_ctx *ctx, const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *weight, int type, int64_t rows,
                      int64_t cols, float eps, void *sum_out, int64_t lds, void *out, int out_type, int64_t ldo, float *out_scale);

@@ -5,7 +5,10 @@
 //   8 bits:   a = max |p|;  out = rint(127 p / a), scale = a * rstd / 127: rstd does not enter the codes, so the sum of squares and the maximum are found
 //             together, by one exchange between the warps.
 //
-// 2048 x 8192 bf16: 25.2 us (134 MB, 5.3 TB/s).
+// A bfloat16 row's squares may leave the binary32 range where the norm does not (above, or below 2^-90 under an eps that would show it).  A warp whose sums come near that
+// takes them again of h 2^-96, or h 2^96, while the row is still in its registers; they count where the row's sum is out of range.
+//
+// 2048 x 8192 bf16: 25.4 us (134 MB, 5.3 TB/s).
 // A row is a block's; its values stay in registers between the sum and the result, so that each is read once and written once.  Bound by those bytes where rows
 // are many, by the chain load - exchange - store where they are few.  Rows too long for the registers are read again.
 #include "skim_grouped.cuh"
@@ -15,6 +18,7 @@ namespace {
 using namespace skimg;
 
 constexpr int MAX_T = 1024;
+constexpr float MOST = 3.402823466e38f, MOST_OF_THREAD = 0x1p108f;       // the greatest finite number; sums of MAX_T threads' stay below it
 
 template <bool BF16>
 __device__ __forceinline__ float value_of(uint32_t h)
@@ -86,6 +90,7 @@ template <bool BF16, bool VEC, int NV>
 __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel(SkimNorm n)
 {
     __shared__ float sums[2][32], tops[2][32];
+    __shared__ float again[BF16 ? 2 : 1][32];                // sums of squares of a warp that may be out of range, of h 2^96 or h 2^-96
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
     skim_wait_for_previous_kernel();
     skim_let_next_kernel_start();
@@ -114,6 +119,16 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
             top = greatest(top, fabsf(p[e]));
         }
     };
+    auto again8 = [&](uint4 x, uint4 r, float by, float sq) {
+        // (whole pieces as if unknown: kept from the first sum the values would cost every row registers; others are not packed on the way)
+        if (VEC) asm volatile("" : "+r"(x.x), "+r"(x.y), "+r"(x.z), "+r"(x.w));
+        float h[8];
+        sum8(x, r, h);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sq = fmaf(h[e] * by, h[e] * by, sq);
+        return sq;
+    };
+    const float least = BF16 && n.eps < 0x1p-70f ? 0x1p-90f : 0.0f;
     constexpr int M = NV ? NV : 1;
     uint4 xs[M], rs[M];
     auto ask = [&](int64_t row) {
@@ -144,7 +159,6 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
                 if (sr) store8<BF16, VEC>(sr, j, n.cols, h);
                 take8(h, p[v], sq, top);
             }
-            if (row + gridDim.x < n.rows) ask(row + gridDim.x);
         } else {
             for (int64_t j = tid * 8; j < n.cols; j += step) {
                 float h[8];
@@ -153,6 +167,26 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
                 take8(h, p[0], sq, top);
             }
         }
+        if constexpr (BF16) {
+            // in range for all threads: so is any sum of them; below it for all: the warp's may be
+            if (__any_sync(0xffffffffu, !(sq >= least && sq <= MOST_OF_THREAD))) {
+                const float by = __any_sync(0xffffffffu, sq > MOST_OF_THREAD) ? 0x1p-96f : 0x1p96f;
+                float d = 0.0f;
+                if constexpr (NV != 0) {
+#pragma unroll
+                    for (int v = 0; v < NV; ++v) {
+                        if (v * step + tid * 8 >= n.cols) break;
+                        d = again8(xs[v], rs[v], by, d);
+                    }
+                } else {
+                    for (int64_t j = tid * 8; j < n.cols; j += step) d = again8(load8<VEC>(x_of(row), j, n.cols), n.residual ? load8<VEC>(r_of(row), j, n.cols) : make_uint4(0u, 0u, 0u, 0u), by, d);
+                }
+#pragma unroll
+                for (int off = 16; off; off >>= 1) d += __shfl_xor_sync(0xffffffffu, d, off);
+                if (lane == 0) again[turn][warp] = d;
+            }
+        }
+        if (NV != 0 && row + gridDim.x < n.rows) ask(row + gridDim.x);
 #pragma unroll
         for (int off = 16; off; off >>= 1) {
             sq += __shfl_xor_sync(0xffffffffu, sq, off);
@@ -170,9 +204,34 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
             sq += __shfl_xor_sync(0xffffffffu, sq, off);
             top = greatest(top, __shfl_xor_sync(0xffffffffu, top, off));
         }
-        const float rstd = 1.0f / sqrtf(sq / (float)n.cols + n.eps);
+        float eps = n.eps, root = 1.0f, lift = 1.0f;         // rstd = root / sqrt(mean + eps), and p takes lift before it: 1 / sqrt may be beyond the range where the result is not
+        if constexpr (BF16) {
+            if (sq < least || sq > MOST) {                   // the same for the whole block.  (One by one: with shuffles here p was spilled)
+                const bool small = sq < least;
+                const float by = small ? 0x1p96f : 0x1p-96f;
+                sq = 0.0f;
+#pragma unroll 1
+                for (int w = 0; w < warps; ++w) {
+                    const float of = sums[turn][w];
+                    sq += of >= least && of <= MOST ? of * by * by : small == (of < least) ? again[turn][w] : 0.0f;
+                }
+                eps = eps * by * by;
+                root = by;
+                if (small && sq / (float)n.cols + eps < 0x1p-8f) {
+                    lift = 0x1p64f;
+                    root = 0x1p32f;
+                    if (NV != 0 && n.out_type != SKIM_TYPE_I8) {         // (8 bits: the codes are of p as it is)
+#pragma unroll
+                        for (int v = 0; v < NV; ++v)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) p[v][e] *= 0x1p64f;
+                    }
+                }
+            }
+        }
+        const float rstd = 1.0f / sqrtf(sq / (float)n.cols + eps) * root;
+        if (n.out_scale && tid == 0) n.out_scale[row] = top * rstd / 127.0f * lift;
         const float by = top > 0.0f ? 127.0f / top : 0.0f;
-        if (n.out_scale && tid == 0) n.out_scale[row] = top * rstd / 127.0f;
         auto result8 = [&](int64_t j, float v[8]) {
             if (n.out_type == SKIM_TYPE_I8) {
                 int8_t *o = static_cast<int8_t *>(n.out) + row * n.ldo;
@@ -188,7 +247,7 @@ __global__ void __launch_bounds__(NV == 4 ? 512 : MAX_T) skim_add_rmsnorm_kernel
                 }
             } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] *= rstd;
+                for (int e = 0; e < 8; ++e) v[e] = (BF16 && NV == 0 ? v[e] * lift : v[e]) * rstd;
                 store8<BF16, VEC>(static_cast<uint16_t *>(n.out) + row * n.ldo, j, n.cols, v);
             }
         };
@@ -214,9 +273,11 @@ template <bool BF16, bool VEC>
 int launch(skim_ctx *ctx, const SkimNorm &n)
 {
     // a warp for every 256 columns; from 2048 columns on more pieces a thread where rows are many.  Many rows are dealt to as many blocks as the SMs hold.
+    // (bfloat16 rows that are no whole pieces: four a thread 140 us, two 116, 2048 x 8191.)
+    constexpr int MOST_PIECES = BF16 && !VEC ? 2 : 4;
     const int64_t pieces = (n.cols + 7) / 8;
     int nv = 1;
-    while (nv < 4 && (pieces > (int64_t)nv * MAX_T || (n.rows > ctx->sm_count && pieces >= (int64_t)nv * 256))) nv *= 2;
+    while (nv < MOST_PIECES && (pieces > (int64_t)nv * MAX_T || (n.rows > ctx->sm_count && pieces >= (int64_t)nv * 256))) nv *= 2;
     if (pieces > (nv == 4 ? 4 * 512 : nv * MAX_T)) nv = 0;
     const int64_t threads = nv ? (pieces + nv - 1) / nv : MAX_T;
     const unsigned block = (unsigned)((threads + 31) / 32 * 32);
@@ -225,7 +286,7 @@ int launch(skim_ctx *ctx, const SkimNorm &n)
     switch (nv) {
     case 1: return skim_launch_dependent(ctx, skim_add_rmsnorm_kernel<BF16, VEC, 1>, grid, block, 0, n);
     case 2: return skim_launch_dependent(ctx, skim_add_rmsnorm_kernel<BF16, VEC, 2>, grid, block, 0, n);
-    case 4: return skim_launch_dependent(ctx, skim_add_rmsnorm_kernel<BF16, VEC, 4>, grid, block, 0, n);
+    case 4: return skim_launch_dependent(ctx, skim_add_rmsnorm_kernel<BF16, VEC, MOST_PIECES>, grid, block, 0, n);
     default: return skim_launch_dependent(ctx, skim_add_rmsnorm_kernel<BF16, VEC, 0>, grid, block, 0, n);
     }
 }
