@@ -317,8 +317,8 @@ int skim_matvec(skim_ctx *ctx, const uint32_t *packed, const int32_t *row_order,
  *          scale's 16 bits, the zero point in the byte above them.
  *   err    out [rows] binary32, may be NULL: sum_j g_ij (x_ij - value_ij)^2 with g the importance (same layout as W; NULL: 1), the
  *          objective that skim_cluster_rows reports.  Summed in binary32 in a fixed order.
- * Needs a workspace of 512 bytes (status word): NaN or Inf in W sets SKIM_STATUS_BAD_WEIGHT, and SKIM_STATUS_BAD_IMPORTANCE as in the clustering.
- * skim_grouped_bytes is a host-only helper.
+ * Needs a workspace of 512 bytes (status word): NaN or Inf in W sets SKIM_STATUS_BAD_WEIGHT, and SKIM_STATUS_BAD_IMPORTANCE as in the clustering, where err
+ * is NULL too.  skim_grouped_bytes is a host-only helper.
  */
 int skim_grouped_bytes(int64_t rows, int64_t cols, int group, size_t *out);
 int skim_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *importance, int64_t rows, int64_t cols, int64_t ld, int group,

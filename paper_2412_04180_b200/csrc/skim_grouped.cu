@@ -28,7 +28,7 @@ struct QuantArgs {
     int ct, record;
     int vec, gvec;           // 16-byte loads of weights, of importances
     unsigned char *tiles;
-    float *err;
+    float *err;              // nullptr: the importances are looked over all the same
     unsigned long long *status;
 };
 
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(QT, 2) skim_grouped_quantize_kernel(QuantArgs 
         err += __shfl_xor_sync(0xffffffffu, err, 2);
         if (p == 0) sums[warp][lane >> 2] = err;
         __syncthreads();
-        if (threadIdx.x < 8 && (int64_t)blockIdx.x * 8 + threadIdx.x < a.rows) {
+        if (a.err && threadIdx.x < 8 && (int64_t)blockIdx.x * 8 + threadIdx.x < a.rows) {
             float v = sums[0][threadIdx.x];
 #pragma unroll
             for (int w = 1; w < QW; ++w) v += sums[w][threadIdx.x];
@@ -305,10 +305,11 @@ int skim_launch_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *
     a.status = (unsigned long long *)ctx->ws;
     const dim3 grid((unsigned)(skim_record_tiles(rows, SKIM_RECORD_ROWS) * 2));     // whole records: rows beyond the last are zeros
     const int per = SKIM_RECORD_COLS / group;
+    const bool with_err = err || importance;
 #define SKIM_QUANT(P)                                                                                                                                  \
-    return rscale ? (err ? skim_launch_dependent(ctx, skim_grouped_quantize_kernel<P, true, true>, grid, QT, 0, a)                                      \
+    return rscale ? (with_err ? skim_launch_dependent(ctx, skim_grouped_quantize_kernel<P, true, true>, grid, QT, 0, a)                                      \
                          : skim_launch_dependent(ctx, skim_grouped_quantize_kernel<P, true, false>, grid, QT, 0, a))                                    \
-                  : (err ? skim_launch_dependent(ctx, skim_grouped_quantize_kernel<P, false, true>, grid, QT, 0, a)                                     \
+                  : (with_err ? skim_launch_dependent(ctx, skim_grouped_quantize_kernel<P, false, true>, grid, QT, 0, a)                                     \
                          : skim_launch_dependent(ctx, skim_grouped_quantize_kernel<P, false, false>, grid, QT, 0, a))
     if (per == 1) { SKIM_QUANT(1); }
     if (per == 2) { SKIM_QUANT(2); }

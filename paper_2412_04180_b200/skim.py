@@ -386,7 +386,8 @@ class Skim:
     def grouped_quantize(self, W, group=128, importance=None, want_err=False, out=None):
         """Uniform 4-bit codes with a scale and a zero point per ``group`` (32, 64 or 128) columns of the float16 matrix W (of W / alpha
         where a scale vector is installed).  Returns dict(tiles uint8, rows, cols, group, err): the stored form, which grouped_dequantize, grouped_matvec
-        and grouped_gated read, and (want_err) the float32 [rows] error, weighted with ``importance`` (float32, like W), else None."""
+        and grouped_gated read, and (want_err) the float32 [rows] error, weighted with ``importance`` (float32, like W), else None.  ``importance`` where
+        there is no error is only looked over (get_status)."""
         rows, cols, ld = self._rows_of(W, "W", (torch.float16,))
         if W.dim() != 2:
             raise TypeError(f"W: expected a matrix, got shape {tuple(W.shape)}")
