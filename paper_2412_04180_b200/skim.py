@@ -387,7 +387,7 @@ class Skim:
         """Uniform 4-bit codes with a scale and a zero point per ``group`` (32, 64 or 128) columns of the float16 matrix W (of W / alpha
         where a scale vector is installed).  Returns dict(tiles uint8, rows, cols, group, err): the stored form, which grouped_dequantize, grouped_matvec
         and grouped_gated read, and (want_err) the float32 [rows] error, weighted with ``importance`` (float32, like W), else None.  ``importance`` where
-        there is no error is only looked over (get_status)."""
+        there is no error is only looked over (get_status).  A result given as ``out`` is filled: its err where it has one, and (want_err) one made for it where not."""
         rows, cols, ld = self._rows_of(W, "W", (torch.float16,))
         if W.dim() != 2:
             raise TypeError(f"W: expected a matrix, got shape {tuple(W.shape)}")
@@ -402,6 +402,8 @@ class Skim:
         if held != [rows, cols, group]:
             raise TypeError(f"out: holds rows, cols, group {held}, expected {[rows, cols, group]}")
         err = out.get("err")
+        if err is None and want_err:
+            err = out["err"] = self._new(torch.float32, rows)
         _chk((_lib or lib()).skim_grouped_quantize(self._h, W.data_ptr(), None if importance is None else importance.data_ptr(), rows, cols, ld, group, tiles,
                                          None if err is None else self._plain(err, "err", torch.float32, rows)), "skim_grouped_quantize")
         return out
