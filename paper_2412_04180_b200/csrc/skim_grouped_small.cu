@@ -368,28 +368,22 @@ int launch(skim_ctx *ctx, const SmallArgs &all)
     if (blocks * a.split > 0x7fffffff) return SKIM_ERR_SHAPE;
     auto kernel = skim_grouped_small_kernel<XT, PER, NREC, NT>;
     static_assert(smem <= 47 * 1024, "no permission needed");
-    constexpr int64_t most = 65535 * (8 * NT);               // tokens of a launch
-    for (int64_t first = 0; first < all.p.tokens; first += most) {
-        a.p.x = static_cast<const unsigned char *>(all.p.x) + first * all.p.ldx * (XT == SKIM_TYPE_I8 ? 1 : 2);
-        a.p.x_scale = all.p.x_scale ? all.p.x_scale + first : nullptr;
-        a.p.out = static_cast<unsigned char *>(all.p.out) + first * all.p.ldo * (all.p.out_type == SKIM_TYPE_F32 ? 4 : 2);
-        a.p.tokens = all.p.tokens - first < most ? all.p.tokens - first : most;
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3((unsigned)(blocks * a.split), (unsigned)((a.p.tokens + 8 * NT - 1) / (8 * NT)));
-        cfg.blockDim = dim3(T);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = ctx->stream;
-        cudaLaunchAttribute attr[2];
-        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[0].val.programmaticStreamSerializationAllowed = 1;
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = (unsigned)a.split;
-        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = a.split > 1 ? 2 : 1;
-        SKIM_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
-        ctx->launches += 1;
-    }
+    static_assert(NT < 2 || 65535ll * (8 * NT) >= SKIM_MAX_TOKENS, "all tokens in one launch (NT = 1 has eight at most)");
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(blocks * a.split), (unsigned)((a.p.tokens + 8 * NT - 1) / (8 * NT)));
+    cfg.blockDim = dim3(T);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = ctx->stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)a.split;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.split > 1 ? 2 : 1;
+    SKIM_CUDA_OK(cudaLaunchKernelEx(&cfg, kernel, a));
+    ctx->launches += 1;
     return SKIM_OK;
 }
 
