@@ -83,7 +83,7 @@ extern "C" {
 #define SKIM_STATUS_BAD_IMPORTANCE 2ull  /* NaN, Inf or negative importance */
 #define SKIM_STATUS_BAD_SCALE 4ull       /* zero, negative or non-finite scale entry */
 #define SKIM_STATUS_BAD_BITS 8ull        /* an allocated width that is not in bit_set (row skipped) */
-#define SKIM_STATUS_TIMEOUT 16ull        /* an asynchronous copy did not complete within its wait limit (row skipped) */
+#define SKIM_STATUS_TIMEOUT 16ull        /* a wait ran out: an asynchronous copy did not complete within its limit (clustering: row skipped; products: results are not complete) */
 #define SKIM_STATUS_BOUNDS 32ull         /* checked build only (-DSKIM_CHECK_BOUNDS): a computed index was out of range (access skipped) */
 
 typedef struct skim_ctx skim_ctx;

@@ -10,8 +10,9 @@
 //
 // Both kernels stream: weights (and importances) in, half a byte a weight out, or the other way round.  A thread has one row's four runs of eight
 // columns of a record, so the group's extremes are two shuffles within a quad, its 16 bytes of codes leave in one store, and a row's error
-// stays in a register until the row ends.  4096 x 11008, groups of 128: quantised with importances in 60 us (294 MB, 4.9 TB/s; 16 warps an SM of 117 registers do not cover
-// the loads), back in 18 us (114 MB, 6.3 TB/s).
+// stays in a register until the row ends.  4096 x 11008, groups of 128: quantised with importances in 62 us (294 MB, 4.7 TB/s; 16 warps an SM of 117 registers do not cover
+// the loads), without 42, with an installed scale vector 83 and 62; back in 19 us (114 MB, 6.0 TB/s).  Rows that do not lie at whole 16-byte pieces are moved element by element, lanes
+// 16 bytes apart, so every instruction touches all the sectors of its span: 4096 x 11007 118 us, without importances 72, back 184.
 #include "skim_grouped.cuh"
 
 namespace {

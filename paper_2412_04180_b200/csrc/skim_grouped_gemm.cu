@@ -9,8 +9,10 @@
 // accumulator holds one group's sum, in binary32, and eight warps take it times the group's scale into binary32 totals in their registers,
 // while the tensor cores are at the next one.
 // Where tiles are few the pairs of a cluster share the columns and add their totals, in a fixed order, through shared memory.
-// Measured: 1024 bf16 tokens 11008 x 4096 86 us (1.07 PFLOP/s, 65 % of the measured peak), gated 300 tokens 22016 x 8192 208 us (1.04 PFLOP/s).  A step of 768 clocks of products takes
-// about 1090: the readback of every group's sums and the stores of operand A go through the same tensor memory.
+// Measured: 1024 bf16 tokens 11008 x 4096 85 us (1.08 PFLOP/s, 65 % of the measured peak), gated 300 tokens 22016 x 8192 207 us (1.05 PFLOP/s).  A step of 768 clocks of products takes
+// 1230: the warp that issues them waits about 480 for an accumulator, of which there are two, and one goes 1480 clocks from the issue to the warps that read it and 400 more until it
+// is free.  The last round of tiles is not full either (258 tiles on 74 pairs), nor the last tile of the tokens.  Groups of 64: 125 us, of 32: 215 us, a round for each of them.  8-bit rows: 109, 173
+// and 301 us, gated 258: their products take half the clocks, but the round is the same and whole sums are converted on top, so the narrower rows are the slower ones here.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

@@ -10,7 +10,8 @@
 // 16-bit activations: a record is m16n8k16 products of exact binary16 (bfloat16) numbers, the codes less their zero point, added in binary32; after every group
 // the sum is taken times the group's scale into the binary32 total.  8-bit activations: m16n8k32 products of the codes themselves in whole numbers, a further one
 // with ones gives the activations' sum, which the zero point takes off.  Eight tokens are the narrow side of the instructions, so one to eight cost the same.
-// Measured, one token: 4096 x 4096 4.3 us (8.9 MB), 4096 x 11008 8.0 us (3.0 TB/s), gated 11008 x 4096 13.6 us (3.5 TB/s; 8-bit rows 11.5 us, 4.2 TB/s).
+// Measured, one token: 4096 x 4096 4.4 us (8.9 MB), 4096 x 11008 8.2 us (2.9 TB/s), gated 11008 x 4096 13.8 us (3.5 TB/s; 8-bit rows 11.5 us, 4.2 TB/s).  A column count that is no multiple
+// of 8 has every record's activations read one by one, for one token too: 4096 x 4097 7.2 us.
 #include <type_traits>
 
 #include "skim_grouped.cuh"
@@ -36,8 +37,9 @@ struct SmallArgs {
 };
 
 // The ring of a warp: `DEPTH` places for a record of each matrix; its activations in registers: SETS, of which one is in use and the others on their way.
-// One matrix: blocks of 8 warps, which share the columns of a row of records (4096 x 4096, one token: 4.7 us, with 4 warps 5.5).  Two matrices: 4 warps, and registers
-// for five blocks of an SM, so that 11008 rows are one round of blocks (11008 x 4096, one token: 13.9 us; with 8 warps 17.9, without the limit 20.6).
+// One matrix: blocks of 8 warps, which share the columns of a row of records (4096 x 4096, one token, when they were chosen: 4.7 us, with 4 warps 5.5).  Two matrices: 4 warps, and
+// registers for five blocks of an SM, so that 11008 rows are one round of blocks (11008 x 4096, one 16-bit token: 13.9 us; with 8 warps 17.9, without the limit 20.6).  For two matrices and
+// 8-bit rows the limit holds at 9 to 16 tokens too, where the instances spill (250 to 430 bytes of stores; 16 tokens 21.1 us): not measured with fewer blocks.
 template <int XT, int PER, int NREC, int NT>
 struct Ring {
     static constexpr int NW = NREC == 1 ? 8 : 4, T = NW * 32, BLOCKS = NREC == 1 ? 2 : NT == 1 || XT == SKIM_TYPE_I8 ? 5 : 3;
@@ -333,8 +335,8 @@ __global__ void __launch_bounds__(Ring<XT, PER, NREC, NT>::T, Ring<XT, PER, NREC
 
 // How the warps share rows and columns, by the clocks of an SM: a warp alone takes about 600 a record (its chain of copies, expansion and products); warps
 // together share the issue slots at about 28 a record, and 60 for the start and the end of each.  A cluster's barriers and sums cost 2500 and 100 a token (gated 300): blocks share columns only
-// where rows are few and long.  (us, kw warps a block and split blocks, measured: 4096 x 4096, one token, 4 warps: kw 4 5.5, kw 2 split 2 6.5, kw 1 split 4 6.8;
-// gated 11008 x 4096: kw 4 13.9, kw 2 15.8, kw 2 split 2 14.8; 128 x 11008, kw 8: alone 6.0, split 4 3.7.)
+// where rows are few and long.  For one matrix the rule counts three blocks an SM, though two are resident.  (us, kw warps a block and split blocks, measured: 4096 x 4096, one
+// token, 4 warps a block: kw 4 5.5, kw 2 split 2 6.5, kw 1 split 4 6.8; gated 11008 x 4096: kw 4 13.9, kw 2 15.8, kw 2 split 2 14.8; 128 x 11008, 8 warps, kw 8: alone 6.0, split 4 3.7.)
 struct Plan {
     int kw, split;
 };
