@@ -323,7 +323,7 @@ int skim_matvec(skim_ctx *ctx, const uint32_t *packed, const int32_t *row_order,
 int skim_grouped_bytes(int64_t rows, int64_t cols, int group, size_t *out);
 int skim_grouped_quantize(skim_ctx *ctx, const uint16_t *W, const float *importance, int64_t rows, int64_t cols, int64_t ld, int group,
                           void *tiles, float *err);
-/* out [rows][ld_out] binary16: the values, rounded once.  No workspace is used. */
+/* out [rows][ld_out] binary16: the values, rounded once (infinite where a scale was rounded up and 15 of it reach 65520).  No workspace is used. */
 int skim_grouped_dequantize(skim_ctx *ctx, const void *tiles, int64_t rows, int64_t cols, int group, uint16_t *out, int64_t ld_out);
 
 /*
